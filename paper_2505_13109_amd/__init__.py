@@ -11,3 +11,4 @@ from .binding import (  # noqa: F401
     FKV_HEADS_ALL, FKV_HEADS_FLAGGED, FKV_HEADS_UNFLAGGED, FKV_RECALL_GATHER, FKV_RECALL_MEMCPY,
     FkvConfig, FreeKV, FreeKVError, lib, lib_path, EXPORTED_SYMBOLS,
 )
+from .paged_cache import PagedCache  # noqa: F401

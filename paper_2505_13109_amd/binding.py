@@ -1,4 +1,4 @@
-"""ctypes binding of include/freekv.h.  Argument marshalling only."""
+"""ctypes binding of include/freekv.h and include/freekv_cache.h.  Argument marshalling only."""
 from __future__ import annotations
 
 import ctypes as C
@@ -25,6 +25,9 @@ EXPORTED_SYMBOLS = (
     "fkv_page_select", "fkv_recall_pages", "fkv_sparse_decode_attn", "fkv_commit",
     "fkv_decode_step", "fkv_flush", "fkv_debug_read", "fkv_debug_read_page", "fkv_profile_enable", "fkv_profile_read", "fkv_profile_attn", "fkv_profile_select", "fkv_profile_launch_floor", "fkv_step_launches", "fkv_export_nhd",
     "fkv_sparse_decode_attn_static", "fkv_recall_pending", "fkv_attach_nhd_pool", "fkv_test_lose_selection", "fkv_test_launch_number", "fkv_test_impatience", "fkv_test_by_itself", "fkv_instrument_timestamps",
+    "fkv_cache_arena_bytes", "fkv_cache_create", "fkv_cache_destroy", "fkv_cache_last_error", "fkv_cache_health", "fkv_cache_used_pages",
+    "fkv_cache_extend", "fkv_cache_append", "fkv_cache_attn", "fkv_cache_read", "fkv_cache_fork", "fkv_cache_copy", "fkv_cache_free",
+    "fkv_cache_compact", "fkv_cache_tables",
 )
 
 
@@ -45,6 +48,10 @@ class FkvConfig(C.Structure):
         ("window_tokens", C.c_int32), ("dtype", C.c_int32), ("placement", C.c_int32),
         ("tau", C.c_float), ("recall_mode", C.c_int32), ("select_pooling", C.c_int32), ("corr_pooling", C.c_int32),
     ]
+
+
+class CacheConfig(C.Structure):
+    _fields_ = [(name, C.c_int32) for name in ("n_layers", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "max_seqs", "max_ctx", "n_pages", "dtype")]
 
 
 def lib_path() -> str:
@@ -101,6 +108,24 @@ def lib() -> C.CDLL:
         "fkv_debug_read": (C.c_int, [vp, i32, i32, vp, sz]),
         "fkv_debug_read_page": (C.c_int, [vp, i32, i32, i32, i32, i32, vp]),
     }
+    cachep = C.POINTER(CacheConfig)
+    sig.update({
+        "fkv_cache_arena_bytes": (C.c_int, [cachep, C.POINTER(sz)]),
+        "fkv_cache_create": (C.c_int, [cachep, vp, sz, C.POINTER(vp)]),
+        "fkv_cache_destroy": (C.c_int, [vp]),
+        "fkv_cache_last_error": (C.c_char_p, [vp]),
+        "fkv_cache_health": (C.c_int, [vp]),
+        "fkv_cache_used_pages": (C.c_int, [vp]),
+        "fkv_cache_extend": (C.c_int, [vp, vp, i32, vp, vp]),
+        "fkv_cache_append": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, i32, vp]),
+        "fkv_cache_attn": (C.c_int, [vp, i32, vp, i32, vp, vp, i32, i32, i32, vp, vp]),
+        "fkv_cache_read": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, i32, vp]),
+        "fkv_cache_fork": (C.c_int, [vp, vp, vp, i32, vp]),
+        "fkv_cache_copy": (C.c_int, [vp, vp, vp, vp, i32, vp]),
+        "fkv_cache_free": (C.c_int, [vp, vp, i32, vp]),
+        "fkv_cache_compact": (C.c_int, [vp, vp]),
+        "fkv_cache_tables": (C.c_int, [vp, vp, i32, vp, vp, vp]),
+    })
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
         fn.restype = res

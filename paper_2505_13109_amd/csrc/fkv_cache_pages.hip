@@ -1,0 +1,395 @@
+// The paged cache's pages: taking them for new tokens, sharing, copying, compacting and giving them back.
+//
+// What is decided (who gets which page, who may be forked to where) is decided by one block that sees the whole call; what is
+// then moved is moved by as many blocks as there is to move.
+#include "fkv_cache.h"
+
+namespace fkv {
+
+namespace {
+
+constexpr int PLAN_THREADS = 1024;
+
+// sum over the threads before this one, and over all of them; the whole block calls it
+__device__ int scan_block(int v, int* total, int* sh) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (int)blockDim.x >> 6;
+  int x = v;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) sh[wave] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int w = 0; w < waves; ++w) {
+    if (w < wave) before += sh[w];
+    all += sh[w];
+  }
+  __syncthreads();
+  *total = all;
+  return before + x - v;
+}
+
+// the first entry that names each slot: first[slot], for entries that name one
+__device__ void first_entries(const int32_t* slots, int n, int max_seqs, int* first) {
+  for (int s = threadIdx.x; s < max_seqs; s += (int)blockDim.x) first[s] = n;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += (int)blockDim.x) {
+    const int s = slots[i];
+    if (s >= 0 && s < max_seqs) atomicMin(&first[s], i);
+  }
+  __syncthreads();
+}
+
+// Takes the `total` lowest free pages of a pool that has as many, and calls got(k, page) for the k-th of them.
+template <typename F>
+__device__ void take_pages(const CacheDesc& c, int total, int* sh, F got) {
+  const int words = (c.n_pages + 31) / 32;
+  int done = 0;
+  for (int w0 = 0; w0 < words && done < total; w0 += (int)blockDim.x) {
+    const int w = w0 + (int)threadIdx.x;
+    uint32_t free_bits = 0, old = 0;
+    if (w < words) {
+      old = c.used[w];
+      free_bits = ~old;
+      if (w == words - 1 && (c.n_pages & 31)) free_bits &= (1u << (c.n_pages & 31)) - 1;
+    }
+    int here;
+    int k = done + scan_block(__popc(free_bits), &here, sh);
+    uint32_t taken = 0;
+    while (free_bits && k < total) {
+      const int b = __ffs((int)free_bits) - 1;
+      free_bits &= free_bits - 1;
+      taken |= 1u << b;
+      const int page = w * 32 + b;
+      c.ref[page] = 1;
+      got(k, page);
+      ++k;
+    }
+    if (taken) c.used[w] = old | taken;
+    done += here;
+  }
+}
+
+// the row whose pages begin at or before the k-th: the last one with off[row] <= k
+__device__ int row_of(const int* off, int n, int k) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (off[mid] <= k) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// One block: lengths grow, and every row gets the pages that its new tokens fill.  LDS: first[max_seqs], off[n_rows].
+__global__ __launch_bounds__(PLAN_THREADS) void cache_extend_kernel(CacheDesc c, const int32_t* __restrict__ seqs, int n_rows,
+                                                                    const int32_t* __restrict__ cu) {
+  extern __shared__ int lds[];
+  __shared__ int sh[PLAN_THREADS / 64];
+  int* const first = lds;
+  int* const off = lds + c.max_seqs;
+  first_entries(seqs, n_rows, c.max_seqs, first);
+
+  constexpr int PER = CACHE_MAX_SEQS / PLAN_THREADS;
+  const int per = (n_rows + PLAN_THREADS - 1) / PLAN_THREADS;
+  int slot[PER], n[PER], len[PER], need[PER], mine = 0, faults = 0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = (int)threadIdx.x * per + j;
+    slot[j] = -1; n[j] = 0; len[j] = 0; need[j] = 0;
+    if (j >= per || i >= n_rows) continue;
+    const int s = seqs[i];
+    const int m = cu ? max(cu[i], 0) : 0;
+    const int t = cu ? cu[i + 1] - m : 1;
+    if (s == -1) continue;
+    if (s < 0 || s >= c.max_seqs || first[s] != i || t < 0) { faults |= FAULT_ENTRY; continue; }
+    slot[j] = s;
+    len[j] = c.len[s];
+    if (t > c.max_pages * PG - len[j]) { faults |= FAULT_RANGE; continue; }
+    n[j] = t;
+    need[j] = (len[j] + t) / PG - len[j] / PG;
+    mine += need[j];
+  }
+  int total;
+  int at = scan_block(mine, &total, sh);
+  const bool room = total <= c.n_pages - c.head[CACHE_USED];
+  if (!room) faults |= FAULT_PAGES;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = (int)threadIdx.x * per + j;
+    if (j < per && i < n_rows) off[i] = at;
+    at += need[j];
+  }
+  if (total && room) {
+    __syncthreads();
+    take_pages(c, total, sh, [&](int k, int page) {
+      const int i = row_of(off, n_rows, k), s = seqs[i];
+      c.table[(size_t)s * c.max_pages + c.len[s] / PG + (k - off[i])] = page;
+    });
+    __syncthreads();      // (the lengths above are the old ones)
+    if (threadIdx.x == 0) c.head[CACHE_USED] += total;
+  }
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int s = slot[j];
+    if (s < 0) continue;
+    const int t = room ? n[j] : 0;
+    c.added[s] = t;
+    c.owner[s] = (int)threadIdx.x * per + j;
+    if (t) {
+      c.len[s] = len[j] + t;
+      c.serial[s] += 1;
+    }
+  }
+  if (faults) atomicOr(&c.head[CACHE_FAULTS], faults);
+}
+
+// One block: which entries of a fork or a copy hold.  They make dst what src is, as far as numbers go; ok[i] is src, or -1.
+// COPY: pages of dst's own, in order, and the list of moves that fills them.
+template <bool COPY>
+__global__ __launch_bounds__(PLAN_THREADS) void cache_fork_kernel(CacheDesc a, const int32_t* __restrict__ src, CacheDesc c,
+                                                                  const int32_t* __restrict__ dst, int n) {
+  extern __shared__ int lds[];
+  __shared__ int sh[PLAN_THREADS / 64];
+  int* const first = lds;
+  int* const off = lds + c.max_seqs;
+  first_entries(dst, n, c.max_seqs, first);
+
+  constexpr int PER = CACHE_MAX_SEQS / PLAN_THREADS;
+  const int per = (n + PLAN_THREADS - 1) / PLAN_THREADS;
+  int s[PER], d[PER], len[PER], mine = 0, faults = 0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = (int)threadIdx.x * per + j;
+    s[j] = d[j] = -1; len[j] = 0;
+    if (j >= per || i >= n) continue;
+    const int from = src[i], to = dst[i];
+    if (from == -1 || to == -1) continue;
+    if (from < 0 || from >= a.max_seqs || to < 0 || to >= c.max_seqs || first[to] != i || c.len[to] != 0) { faults |= FAULT_ENTRY; continue; }
+    len[j] = a.len[from];
+    if (COPY && len[j] > c.max_pages * PG) { faults |= FAULT_RANGE; len[j] = 0; continue; }
+    s[j] = from; d[j] = to;
+    mine += len[j] / PG;
+  }
+  int total = 0, at = 0;
+  bool room = true;
+  if (COPY) {
+    at = scan_block(mine, &total, sh);
+    room = total <= c.n_pages - c.head[CACHE_USED];
+    if (!room) faults |= FAULT_PAGES;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = (int)threadIdx.x * per + j;
+      if (j < per && i < n) off[i] = at;
+      at += s[j] >= 0 ? len[j] / PG : 0;
+    }
+    __syncthreads();
+    if (total && room) {
+      take_pages(c, total, sh, [&](int k, int page) {
+        const int i = row_of(off, n, k), pos = k - off[i];
+        c.table[(size_t)dst[i] * c.max_pages + pos] = page;
+        c.from[k] = a.table[(size_t)src[i] * a.max_pages + pos];
+        c.to[k] = page;
+      });
+      __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+      if (room) c.head[CACHE_USED] += total;
+      c.head[CACHE_MOVES] = room ? total : 0;
+    }
+  } else {
+    __syncthreads();      // (every length has been read)
+  }
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = (int)threadIdx.x * per + j;
+    if (j >= per || i >= n) continue;
+    c.ok[i] = room ? s[j] : -1;
+    if (s[j] < 0 || !room) continue;
+    c.len[d[j]] = len[j];
+    c.added[d[j]] = 0;
+    c.owner[d[j]] = -1;
+  }
+  if (faults) atomicOr(&c.head[CACHE_FAULTS], faults);
+}
+
+// copies n 16-byte words, all the block's threads
+__device__ __forceinline__ void copy_words(const void* from, void* to, int n) {
+  const uint4* const f = static_cast<const uint4*>(from);
+  uint4* const t = static_cast<uint4*>(to);
+  for (int i = threadIdx.x; i < n; i += (int)blockDim.x) t[i] = f[i];
+}
+
+// Open pages of the entries that hold; for a fork also its page table, every page of which gets one more owner.
+// grid (layers x heads, and blocks of 1024 table entries for a fork; entries)
+__global__ __launch_bounds__(256) void cache_open_kernel(CacheDesc a, CacheDesc c, const int32_t* __restrict__ dst, bool share) {
+  const int i = blockIdx.y, s = c.ok[i];
+  if (s < 0) return;
+  const int d = dst[i], len = c.len[d], heads = c.n_layers * c.n_kv;      // (src may be some other entry's dst: what counts is what it was)
+  const int x = blockIdx.x;
+  if (x >= heads) {
+    const int pages = len / PG;
+    for (int p = (x - heads) * 1024 + (int)threadIdx.x; p < min(pages, (x - heads + 1) * 1024); p += 256) {
+      const int page = a.table[(size_t)s * a.max_pages + p];
+      c.table[(size_t)d * c.max_pages + p] = page;
+      if (share) atomicAdd(&c.ref[page], 1);
+    }
+    return;
+  }
+  const int rest = len % PG, layer = x / c.n_kv, m = x % c.n_kv;
+  if (!rest) return;
+  const uint16_t* const f = a.open + a.open_at(layer, s, m);
+  uint16_t* const t = c.open + c.open_at(layer, d, m);
+  copy_words(f, t, rest * D / 8);
+  copy_words(f + PG * D, t + PG * D, PG * D / 8);
+}
+
+// Carries the list of moves out, pages of `from` to pages of `to` in all layers; where the pages keep their owners (compact),
+// their counts move too.  Bound by memory.  grid: any number of blocks
+__global__ __launch_bounds__(256) void cache_move_kernel(CacheDesc a, CacheDesc c, bool owners) {
+  const int moves = c.head[CACHE_MOVES];
+  const int words = c.n_kv * CU_BYTES / 16;
+  for (long i = blockIdx.x; i < (long)moves * c.n_layers; i += gridDim.x) {
+    const int layer = (int)(i / moves), k = (int)(i % moves);
+    const int f = c.from[k], t = c.to[k];
+    copy_words(a.units + a.unit(layer, f, 0) * CU_BYTES, c.units + c.unit(layer, t, 0) * CU_BYTES, words);
+    if ((int)threadIdx.x < c.n_kv) c.exps[c.unit(layer, t, threadIdx.x)] = a.exps[a.unit(layer, f, threadIdx.x)];
+    if (owners && layer == 0 && threadIdx.x == 0) {
+      c.ref[t] = c.ref[f];
+      c.ref[f] = 0;
+    }
+  }
+}
+
+// One block: used pages behind the first `pages in use` go to the free places before that, in order.
+__global__ __launch_bounds__(PLAN_THREADS) void cache_compact_kernel(CacheDesc c) {
+  __shared__ int sh[PLAN_THREADS / 64];
+  const int live = c.head[CACHE_USED], words = (c.n_pages + 31) / 32;
+  int holes = 0;
+  for (int w0 = 0; w0 < (live + 31) / 32; w0 += PLAN_THREADS) {
+    const int w = w0 + (int)threadIdx.x;
+    uint32_t bits = 0;
+    if (w * 32 < live) {
+      bits = ~c.used[w];
+      if (live - w * 32 < 32) bits &= (1u << (live - w * 32)) - 1;
+    }
+    int here;
+    int k = holes + scan_block(__popc(bits), &here, sh);
+    for (; bits; bits &= bits - 1, ++k) c.to[k] = w * 32 + __ffs((int)bits) - 1;
+    holes += here;
+  }
+  __syncthreads();
+  int moved = 0;
+  for (int w0 = live / 32; w0 < words; w0 += PLAN_THREADS) {
+    const int w = w0 + (int)threadIdx.x;
+    uint32_t bits = 0;
+    if (w < words) {
+      bits = c.used[w];
+      if (w * 32 < live) bits &= ~((1u << (live - w * 32)) - 1);
+    }
+    int here;
+    int k = moved + scan_block(__popc(bits), &here, sh);
+    for (; bits; bits &= bits - 1, ++k) {
+      const int page = w * 32 + __ffs((int)bits) - 1;
+      c.from[k] = page;
+      c.remap[page] = c.to[k];
+    }
+    moved += here;
+  }
+  __syncthreads();
+  for (int w = threadIdx.x; w < words; w += PLAN_THREADS)
+    c.used[w] = w * 32 >= live ? 0u : live - w * 32 >= 32 ? ~0u : (1u << (live - w * 32)) - 1;
+  if (threadIdx.x == 0) c.head[CACHE_MOVES] = moved;
+}
+
+// Page tables after a compaction: pages behind the ones in use have new numbers.  grid (blocks of 1024 entries, slots)
+__global__ __launch_bounds__(256) void cache_remap_kernel(CacheDesc c) {
+  const int slot = blockIdx.y, live = c.head[CACHE_USED];
+  if (!c.head[CACHE_MOVES]) return;
+  const int pages = c.len[slot] / PG;
+  for (int p = blockIdx.x * 1024 + (int)threadIdx.x; p < min(pages, ((int)blockIdx.x + 1) * 1024); p += 256) {
+    int32_t* const e = c.table + (size_t)slot * c.max_pages + p;
+    if (*e >= live) *e = c.remap[*e];
+  }
+}
+
+// A block per entry: its sequence's pages lose an owner.
+__global__ __launch_bounds__(256) void cache_free_kernel(CacheDesc c, const int32_t* __restrict__ seqs) {
+  const int i = blockIdx.x, s = seqs[i];
+  __shared__ int freed;
+  if (s < 0 || s >= c.max_seqs) {
+    if (s != -1 && threadIdx.x == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
+    return;
+  }
+  bool again = false;
+  for (int j = threadIdx.x; j < i; j += 256) again |= seqs[j] == s;
+  if (threadIdx.x == 0) freed = 0;
+  if (__syncthreads_or(again)) {
+    if (threadIdx.x == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
+    return;
+  }
+  const int pages = c.len[s] / PG;
+  int mine = 0;
+  for (int p = threadIdx.x; p < pages; p += 256) {
+    const int page = c.table[(size_t)s * c.max_pages + p];
+    if (atomicSub(&c.ref[page], 1) == 1) {
+      atomicAnd(&c.used[page >> 5], ~(1u << (page & 31)));
+      ++mine;
+    }
+  }
+  if (mine) atomicAdd(&freed, mine);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    if (freed) atomicSub(&c.head[CACHE_USED], freed);
+    c.len[s] = 0;
+    c.added[s] = 0;
+    c.owner[s] = -1;
+  }
+}
+
+// grid (blocks of 1024 entries, rows)
+__global__ __launch_bounds__(256) void cache_tables_kernel(CacheDesc c, const int32_t* __restrict__ seqs, int32_t* __restrict__ lens,
+                                                           int32_t* __restrict__ pages) {
+  const int i = blockIdx.y, s = seqs[i];
+  const bool there = s >= 0 && s < c.max_seqs;
+  const int len = there ? c.len[s] : 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    lens[i] = len;
+    if (!there && s != -1) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
+  }
+  for (int p = blockIdx.x * 1024 + (int)threadIdx.x; p < min(c.max_pages, ((int)blockIdx.x + 1) * 1024); p += 256)
+    pages[(size_t)i * c.max_pages + p] = p < len / PG ? c.table[(size_t)s * c.max_pages + p] : -1;
+}
+
+}  // namespace
+
+void launch_cache_extend(const CacheDesc& c, const int32_t* seqs, int n_rows, const int32_t* cu, hipStream_t st) {
+  cache_extend_kernel<<<1, PLAN_THREADS, (size_t)(c.max_seqs + n_rows) * 4, st>>>(c, seqs, n_rows, cu);
+}
+
+void launch_cache_fork(const CacheDesc& c, const int32_t* src, const int32_t* dst, int n, hipStream_t st) {
+  cache_fork_kernel<false><<<1, PLAN_THREADS, (size_t)(c.max_seqs + n) * 4, st>>>(c, src, c, dst, n);
+  cache_open_kernel<<<dim3(c.n_layers * c.n_kv + (c.max_pages + 1023) / 1024, n), 256, 0, st>>>(c, c, dst, true);
+}
+
+constexpr int MOVE_BLOCKS = 2048;
+
+void launch_cache_copy(const CacheDesc& from, const int32_t* src, const CacheDesc& to, const int32_t* dst, int n, hipStream_t st) {
+  cache_fork_kernel<true><<<1, PLAN_THREADS, (size_t)(to.max_seqs + n) * 4, st>>>(from, src, to, dst, n);
+  cache_move_kernel<<<MOVE_BLOCKS, 256, 0, st>>>(from, to, false);
+  cache_open_kernel<<<dim3(to.n_layers * to.n_kv, n), 256, 0, st>>>(from, to, dst, false);
+}
+
+void launch_cache_free(const CacheDesc& c, const int32_t* seqs, int n, hipStream_t st) { cache_free_kernel<<<n, 256, 0, st>>>(c, seqs); }
+
+void launch_cache_compact(const CacheDesc& c, hipStream_t st) {
+  cache_compact_kernel<<<1, PLAN_THREADS, 0, st>>>(c);
+  cache_move_kernel<<<MOVE_BLOCKS, 256, 0, st>>>(c, c, true);
+  cache_remap_kernel<<<dim3((c.max_pages + 1023) / 1024, c.max_seqs), 256, 0, st>>>(c);
+}
+
+void launch_cache_tables(const CacheDesc& c, const int32_t* seqs, int n_rows, int32_t* lens, int32_t* pages, hipStream_t st) {
+  cache_tables_kernel<<<dim3((c.max_pages + 1023) / 1024, n_rows), 256, 0, st>>>(c, seqs, lens, pages);
+}
+
+}  // namespace fkv

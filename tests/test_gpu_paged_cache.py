@@ -1,0 +1,733 @@
+"""The paged cache in 4 bits against a plain model in 64 bits (paged_model.py): contents, attention, pages, refusals, graphs."""
+import math
+import random
+
+import pytest
+import torch
+
+from paged_model import D, PG, Model, attention
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"fp16": torch.float16, "bf16": torch.bfloat16}
+
+
+def ints(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def offsets(lens):
+    at = [0]
+    for n in lens:
+        at.append(at[-1] + n)
+    return ints(at)
+
+
+def tokens(gen, n, kv, dtype, make=None):
+    x = torch.randn((2, n, kv, D), generator=gen)
+    x[..., [7, 43, 71, 101]] *= 8
+    if make is not None:
+        x = make(x, gen)
+    x = x.to(TYPES[dtype])
+    return x[0], x[1]
+
+
+class Pair:
+    """A cache and its model, fed with the same."""
+
+    def __init__(self, *, n_layers=1, n_kv=2, G=2, max_seqs=4, max_ctx=512, n_pages=64, dtype="bf16", seed=0):
+        import paper_2505_13109_amd as fkv
+        self.shape = dict(n_layers=n_layers, max_seqs=max_seqs, max_ctx=max_ctx, n_pages=n_pages)
+        self.c = fkv.PagedCache(n_q_heads=n_kv * G, n_kv_heads=n_kv, dtype=dtype, **self.shape)
+        self.m = Model(n_kv=n_kv, dtype=TYPES[dtype], **self.shape)
+        self.kv, self.G, self.dtype, self.layers = n_kv, G, dtype, n_layers
+        self.gen = torch.Generator().manual_seed(seed)
+
+    def grow(self, seqs, new, make=None, uniform=False):
+        """`new` more tokens for each of the slots, in every layer"""
+        cu = None if uniform else offsets(new)
+        self.c.extend(ints(seqs), cu)
+        assert self.m.extend(seqs, new)
+        for layer in range(self.layers):
+            k, v = tokens(self.gen, sum(new), self.kv, self.dtype, make)
+            self.c.append(layer, ints(seqs), k.cuda(), v.cuda(), cu)
+            self.m.append(layer, seqs, new, k, v)
+
+    def read(self, layer, seqs, lens=None):
+        lens = [self.m.len[s] for s in seqs] if lens is None else lens
+        shape = (sum(lens), self.kv, D)
+        k, v = (torch.full(shape, 77.0, dtype=TYPES[self.dtype], device="cuda") for _ in "kv")
+        self.c.read(layer, ints(seqs), k, v, offsets(lens))
+        return k.cpu(), v.cpu()
+
+    def check_contents(self, seqs=None):
+        """Values: one rounding to T of a sum in fp32 whose terms are lo and step times code."""
+        seqs = range(len(self.m.len)) if seqs is None else seqs
+        seqs = [s for s in seqs if self.m.len[s]]
+        half = torch.finfo(TYPES[self.dtype]).eps / 2
+        tiny = float(torch.finfo(TYPES[self.dtype]).smallest_normal) * half
+        for layer in range(self.layers):
+            got = self.read(layer, seqs)
+            at = 0
+            for s in seqs:
+                n = self.m.len[s]
+                value, lo, step = self.m.values(layer, s)
+                for i in (0, 1):
+                    a, b = got[i][at:at + n].double(), value[:, i]
+                    assert torch.equal(a.isnan(), b.isnan()), (layer, s, "kv"[i], "NaN")
+                    off = (a - b).abs()
+                    tol = half * 1.001 * b.abs() + 2.0 ** -23 * (lo[:, i].abs() + 15 * step[:, i]) + tiny
+                    over = torch.isfinite(b) & ~(off <= tol) & ~(b.abs() > torch.finfo(TYPES[self.dtype]).max)
+                    assert not over.any(), (layer, s, "kv"[i], over.nonzero()[0].tolist(), float(off[over].max()))
+                at += n
+
+    def check_tables(self):
+        n = len(self.m.len)
+        lens, pages = ints([-5] * n), torch.full((n, self.m.max_ctx // PG), -5, dtype=torch.int32, device="cuda")
+        self.c.tables(ints(list(range(n))), lens, pages)
+        assert lens.tolist() == self.m.len
+        for s, ids in enumerate(pages.tolist()):
+            assert ids == self.m.pages[s] + [-1] * (len(ids) - len(self.m.pages[s])), s
+        assert self.c.used_pages() == self.m.used()
+        self.c.health()
+
+    def queries(self, rows, scale=1.0):
+        return (torch.randn((rows, self.kv * self.G, D), generator=self.gen) * scale).to(TYPES[self.dtype])
+
+    def check_attention(self, layer, seqs, lists=None, sink=0, window=0, scale=1.0, q=None, got=None):
+        q = self.queries(len(seqs), scale) if q is None else q
+        if got is None:
+            out = torch.full(q.shape, 77.0, dtype=q.dtype, device="cuda")
+            at = None if lists is None else torch.tensor(lists, dtype=torch.int32, device="cuda").view(len(seqs), self.kv, -1)
+            self.c.attn(layer, ints(seqs), q.cuda(), out, pages=at, sink=sink, window=window)
+            got = out.cpu()
+        half = torch.finfo(q.dtype).eps / 2
+        known = {}
+        for r, s in enumerate(seqs):
+            if s < 0:
+                assert not got[r].any()
+                continue
+            if s not in known:
+                known[s] = self.m.values(layer, s)
+            for h in range(self.kv):
+                at = self.m.attended(s, h, None if lists is None else lists[r][h], sink, window)
+                a = [x[at][:, :, h] for x in known[s]]
+                ref, tol = attention(q[r, h * self.G:(h + 1) * self.G], *a, half)
+                off = (got[r, h * self.G:(h + 1) * self.G].double() - ref).abs()
+                assert (off <= tol).all(), (r, s, h, self.m.len[s], float((off / tol.clamp(min=1e-30)).max()), float(off.max()))
+        return got
+
+
+# ---- contents ---------------------------------------------------------------------------------------
+
+def constant(x, gen):
+    x[..., ::3] = x[:, :1, :, ::3]                       # channels that do not change: a step of 0
+    return x
+
+
+def grid(x, gen):
+    return torch.round(x * 2)                            # quotients that lie at a border between two codes
+
+
+def wide(x, gen):
+    e = torch.randint(-60, 60, x.shape[-1:], generator=gen).float()
+    return x * torch.exp2(e)                             # channels of sizes that no fp16 number could tell
+
+
+def offset(x, gen):
+    return x * 0.01 + 100.0                              # a minimum that is much larger than the step
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("make", [None, constant, grid, offset])
+def test_contents_of_sequences_of_all_lengths(dtype, make):
+    p = Pair(n_layers=2, n_kv=3, max_seqs=10, max_ctx=256, n_pages=80, dtype=dtype)
+    p.grow([0, 1, 2, 3, 4, 5, 6, 7, 8], [1, 2, 31, 32, 33, 63, 64, 65, 255], make)
+    p.check_contents()
+    p.check_tables()
+
+
+def test_contents_of_channels_of_very_different_sizes():
+    p = Pair(n_kv=2, max_seqs=2, dtype="bf16")
+    p.grow([0], [100], wide)
+    p.check_contents()
+
+
+def test_contents_at_the_ends_of_the_types():
+    for dtype, top in (("bf16", 3.0e38), ("fp16", 65504.0)):
+        p = Pair(n_kv=1, max_seqs=1, dtype=dtype, seed=3)
+        p.grow([0], [64], lambda x, gen: torch.sign(x) * top * torch.rand(x.shape, generator=gen))
+        p.check_contents()
+    p = Pair(n_kv=1, max_seqs=1, dtype="bf16", seed=4)
+    p.grow([0], [64], lambda x, gen: x * 2.0 ** -120)
+    p.check_contents()
+    p = Pair(n_kv=1, max_seqs=1, dtype="fp16", seed=4)
+    p.grow([0], [64], lambda x, gen: x * 2.0 ** -18)     # denormal fp16 numbers among them
+    p.check_contents()
+
+
+def test_a_channel_that_is_not_finite_is_nan_in_its_page_only():
+    def bad(x, gen):
+        x[0, 5, 0, 10] = math.nan
+        x[1, 40, 1, 20] = math.inf
+        x[1, 70, 1, 21] = -math.inf                      # (token 70 stays in the open page, as it is)
+        return x
+
+    p = Pair(n_kv=2, max_seqs=1)
+    p.grow([0], [80], bad)
+    k, v = p.read(0, [0])
+    assert k[:32, 0, 10].isnan().all() and int(k.isnan().sum()) == 32
+    assert v[32:64, 1, 20].isnan().all() and int(v.isnan().sum()) == 32
+    assert v[70, 1, 21] == -math.inf
+    p.check_contents()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_tokens_one_by_one_and_in_pieces_give_the_same(dtype):
+    """A page's codes do not depend on how its tokens came."""
+    p = Pair(n_layers=2, n_kv=2, max_seqs=4, max_ctx=256, dtype=dtype)
+    for step in range(70):
+        p.grow([0, 2], [1, 1], uniform=True)
+    for n in (5, 40, 3, 64, 16, 32, 95):
+        p.grow([1, 3], [n, 1])
+    p.check_contents()
+    p.check_tables()
+    # the same tokens at once
+    whole = Pair(n_layers=2, n_kv=2, max_seqs=4, max_ctx=256, dtype=dtype)
+    n = p.m.len[1]
+    whole.c.extend(ints([2]), offsets([n]))
+    for layer in range(2):
+        x = p.m.tokens[layer][1]
+        whole.c.append(layer, ints([2]), x[:, 0].contiguous().cuda(), x[:, 1].contiguous().cuda(), offsets([n]))
+        whole.m.len[2] = n
+        a, b = p.read(layer, [1]), whole.read(layer, [2])
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    whole.c.health()
+
+
+def test_read_leaves_what_is_behind_a_sequence_as_it_was():
+    p = Pair(n_kv=2, max_seqs=4)
+    p.grow([0, 2], [45, 70])
+    lens = [50, 20, 10, 64]                              # longer than slot 0, empty, part of a page, up to a page's end
+    k, v = p.read(0, [0, 1, 2, 2], lens)
+    a, _ = p.read(0, [0])
+    b, _ = p.read(0, [2])
+    assert torch.equal(k[:45], a) and (k[45:70] == 77).all() and torch.equal(k[70:80], b[:10]) and torch.equal(k[80:], b[:64])
+    p.c.health()
+    one_k, one_v = (torch.zeros((2, 2, D), dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    p.c.read(0, ints([2, -1]), one_k, one_v)             # one token a row; padding
+    assert torch.equal(one_k[0].cpu(), b[0]) and not one_k[1].any()
+
+
+# ---- attention ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("kv,G", [(1, 1), (2, 3), (8, 4), (4, 7), (2, 8), (1, 16)])
+def test_attention_over_sequences_of_all_lengths(kv, G, dtype):
+    p = Pair(n_layers=2, n_kv=kv, G=G, max_seqs=12, max_ctx=1024, n_pages=128, dtype=dtype)
+    p.grow([0, 1, 2, 3, 4, 5, 6, 7, 8], [1, 2, 31, 32, 33, 64, 65, 300, 1000])
+    p.check_attention(0, [3])
+    p.check_attention(1, [8])
+    p.check_attention(1, [8, -1, 0, 11, 1, 2, 3, 4, 5, 6, 7, 8])      # padding, an empty slot, one twice
+    p.c.health()
+
+
+@pytest.mark.parametrize("scale", [0.0, 0.05, 20.0])
+def test_attention_flat_and_peaked(scale):
+    p = Pair(n_kv=2, G=4, max_seqs=2, max_ctx=2048, n_pages=64)
+    p.grow([0], [1501])
+    p.check_attention(0, [0], scale=scale)
+
+
+def test_attention_where_the_maximum_moves_up_page_by_page():
+    """Every page's logits pass those before by more than the headroom."""
+    p = Pair(n_kv=1, G=4, max_seqs=1, max_ctx=1024, n_pages=32)
+    ramp = lambda x, gen: torch.ones_like(x) * (torch.arange(x.shape[1]).view(1, -1, 1, 1) / 32.0) * torch.tensor([1.0, 0.0]).view(2, 1, 1, 1) + x * 0.1
+    p.grow([0], [900], ramp)
+    q = torch.ones((1, 4, D)) * torch.tensor([1.0, 3.0, -1.0, -3.0]).view(1, 4, 1)
+    p.check_attention(0, [0], q=q.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attention_of_channels_of_very_different_sizes(dtype):
+    """Keys whose channels' steps span more than fp16 holds, queries that make up for it."""
+    p = Pair(n_kv=1, G=2, max_seqs=1, max_ctx=256, dtype=dtype)
+    e = torch.arange(D) % 12 - 6.0
+    p.grow([0], [200], lambda x, gen: x * torch.stack((torch.exp2(e), torch.ones(D))).view(2, 1, 1, D))
+    q = (torch.randn((1, 2, D), generator=p.gen) * torch.exp2(-e)).to(TYPES[dtype])
+    p.check_attention(0, [0], q=q)
+
+
+def test_attention_over_listed_pages():
+    p = Pair(n_kv=2, G=4, max_seqs=4, max_ctx=1024, n_pages=128)
+    p.grow([0, 1, 2], [1000, 96, 37])
+    rng = random.Random(2)
+    rows = [0, 1, 2, 3, 0, -1][:4]
+    lists = []
+    for r, s in enumerate(rows):
+        lists.append([sorted(rng.sample(range(2, 28), 9)) + [-1] * 3 for _ in range(2)])
+    p.check_attention(0, rows, lists, sink=64, window=96)
+    p.check_attention(0, rows, lists)
+    # entries that are none: behind the sequence, in the sink, in the window, below -1; one page twice
+    odd = [[[0, 1, 5, 5, 30, 31, 2000000000, -7, 29, 27, 3, -1]] * 2] * 4
+    p.check_attention(0, rows, odd, sink=64, window=96)
+    p.c.health()
+
+
+def test_attention_with_lists_that_leave_nothing():
+    p = Pair(n_kv=2, G=2, max_seqs=3, max_ctx=256)
+    p.grow([0, 1], [128, 130])
+    none = [[[-1] * 5] * 2] * 2
+    got = p.check_attention(0, [0, 1], none)
+    assert not got[0].any() and got[1].any()             # slot 1 has two tokens in its open page
+    q = p.queries(2)
+    out = torch.full(q.shape, 9.0, dtype=q.dtype, device="cuda")
+    p.c.attn(0, ints([0, 1]), q.cuda(), out, pages=torch.empty((2, 2, 0), dtype=torch.int32, device="cuda"), sink=32, window=32)
+    p.check_attention(0, [0, 1], [[[]] * 2] * 2, sink=32, window=32, q=q, got=out.cpu())
+
+
+def test_attention_cut_into_many_splits():
+    """One head, one row, 20000 tokens: as many splits as there are; then rows of very different lengths together."""
+    p = Pair(n_kv=1, G=5, max_seqs=40, max_ctx=20480, n_pages=900)
+    p.grow([0], [20001])
+    p.check_attention(0, [0])
+    p.grow(list(range(1, 40)), [1 + 7 * i for i in range(39)])
+    p.check_attention(0, list(range(40)))
+
+
+def test_attention_is_the_same_every_time():
+    """Splits are joined in their order whichever ends last."""
+    p = Pair(n_kv=2, G=4, max_seqs=3, max_ctx=8192, n_pages=600)
+    p.grow([0, 1, 2], [8000, 5000, 33])
+    q = p.queries(3).cuda()
+    first = torch.empty_like(q)
+    p.c.attn(0, ints([0, 1, 2]), q, first)
+    for _ in range(20):
+        again = torch.empty_like(q)
+        p.c.attn(0, ints([0, 1, 2]), q, again)
+        assert torch.equal(first, again)
+
+
+def test_attention_of_a_nan_reaches_its_row_and_channel_only():
+    def bad(x, gen):
+        x[1, 5, 0, 10] = math.nan
+        return x
+
+    p = Pair(n_kv=2, G=2, max_seqs=2)
+    p.grow([0], [70], bad)
+    p.grow([1], [70])
+    q = p.queries(2).cuda()
+    out = torch.empty_like(q)
+    p.c.attn(0, ints([0, 1]), q, out)
+    nan = out.isnan()
+    assert nan[0, :2, 10].all() and int(nan.sum()) == 2
+
+
+def test_open_pages_of_others_do_not_matter():
+    """What a slot's open page held before -- here NaN -- is not seen behind its new tokens."""
+    p = Pair(n_kv=1, G=2, max_seqs=1)
+    nan = torch.full((30, 1, D), math.nan, dtype=torch.bfloat16, device="cuda")
+    p.c.extend(ints([0]), offsets([30]))
+    p.c.append(0, ints([0]), nan, nan, offsets([30]))
+    p.c.free(ints([0]))
+    p.grow([0], [3])
+    p.check_attention(0, [0])
+    p.grow([0], [33])
+    p.check_attention(0, [0])
+    p.check_contents()
+
+
+# ---- pages ---------------------------------------------------------------------------------------------
+
+def test_fork_shares_pages_and_parts_where_the_branches_do():
+    p = Pair(n_layers=2, n_kv=2, max_seqs=6, max_ctx=256, n_pages=40)
+    p.grow([0, 1], [100, 64])
+    p.c.fork(ints([0, 0, 1, 5]), ints([2, 3, 4, -1]))
+    p.m.fork([0, 0, 1], [2, 3, 4])
+    p.check_tables()
+    assert p.m.used() == 3 + 2
+    p.check_contents()
+    p.grow([2, 3, 4, 0], [40, 1, 1, 30])
+    p.check_contents()
+    p.check_attention(0, [0, 2, 3, 4, 1])
+    p.c.free(ints([0, 2]))
+    p.m.free([0, 2])
+    p.check_tables()
+    p.check_contents()
+    p.check_attention(1, [3, 4, 1])
+
+
+def test_compact_and_copy_keep_what_sequences_hold():
+    p = Pair(n_layers=3, n_kv=2, max_seqs=8, max_ctx=512, n_pages=70)
+    for _ in range(6):
+        p.grow([0, 1, 2, 3], [40, 33, 50, 17])
+    p.c.fork(ints([3]), ints([4]))
+    p.m.fork([3], [4])
+    p.c.free(ints([0, 2]))
+    p.m.free([0, 2])
+    p.check_tables()
+    before = [p.read(layer, [1, 3, 4]) for layer in range(3)]
+    p.c.compact()
+    p.m.compact()
+    p.check_tables()
+    assert max(max(ids, default=-1) for ids in p.m.pages) == p.m.used() - 1
+    for layer in range(3):
+        after = p.read(layer, [1, 3, 4])
+        assert torch.equal(before[layer][0], after[0]) and torch.equal(before[layer][1], after[1])
+    p.c.compact()                                        # nothing to do
+    p.check_tables()
+    p.c.copy(ints([4, 1]), ints([5, 6]))
+    assert p.m.copy([4, 1], [5, 6])
+    p.check_tables()
+    p.check_contents()
+    p.grow([5, 4, 3], [20, 20, 20])
+    p.check_contents()
+    # a larger pool takes over
+    big = Pair(n_layers=3, n_kv=2, max_seqs=9, max_ctx=1024, n_pages=200)
+    big.grow([8], [70])
+    p.c.copy(ints([4, 6]), ints([0, 7]), to=big.c)
+    assert p.m.copy([4, 6], [0, 7], to=big.m)
+    big.check_tables()
+    big.check_contents()
+    big.grow([0, 7], [300, 1])
+    big.check_contents()
+    p.check_tables()
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_any_order_of_operations(seed):
+    """A run of them as a scheduler would make it, small pool, against the model."""
+    rng = random.Random(seed)
+    dtype = rng.choice(["bf16", "fp16"])
+    p = Pair(n_layers=rng.choice([1, 2]), n_kv=rng.choice([1, 2, 3]), G=rng.choice([1, 2, 4]), max_seqs=8, max_ctx=320, n_pages=44, dtype=dtype, seed=seed)
+    for _ in range(60):
+        live = [s for s in range(8) if p.m.len[s]]
+        idle = [s for s in range(8) if not p.m.len[s]]
+        what = rng.choice(["grow", "grow", "grow", "step", "step", "fork", "copy", "free", "compact", "attn"])
+        if what in ("grow", "step"):
+            seqs = rng.sample(range(8), rng.randint(1, 4)) if what == "grow" else live
+            new = [rng.choice([1, 5, 31, 32, 33, 70]) if what == "grow" else 1 for _ in seqs]
+            ok = [i for i, s in enumerate(seqs) if p.m.len[s] + new[i] <= 320]
+            seqs, new = [seqs[i] for i in ok], [new[i] for i in ok]
+            if seqs and sum((p.m.len[s] + n) // PG - p.m.len[s] // PG for s, n in zip(seqs, new)) <= p.m.ref.count(0):
+                p.grow(seqs, new, uniform=what == "step")
+        elif what == "fork" and live and idle:
+            dst = rng.sample(idle, rng.randint(1, len(idle)))
+            src = [rng.choice(live) for _ in dst]
+            p.c.fork(ints(src), ints(dst))
+            p.m.fork(src, dst)
+        elif what == "copy" and live and idle:
+            dst = rng.sample(idle, 1)
+            src = [rng.choice(live)]
+            if len(p.m.pages[src[0]]) <= p.m.ref.count(0):
+                p.c.copy(ints(src), ints(dst))
+                assert p.m.copy(src, dst)
+        elif what == "free" and live:
+            seqs = rng.sample(live, rng.randint(1, len(live)))
+            p.c.free(ints(seqs))
+            p.m.free(seqs)
+        elif what == "compact":
+            p.c.compact()
+            p.m.compact()
+        elif what == "attn" and live:
+            p.check_attention(rng.randrange(p.layers), rng.sample(range(8), 5))
+        p.check_tables()
+    p.check_contents()
+
+
+def test_many_pages_are_taken_in_order():
+    """More than one pass over the bits of free pages: 40000 of them, every third sequence given back."""
+    p = Pair(n_layers=1, n_kv=1, G=1, max_seqs=600, max_ctx=2176, n_pages=40000)
+    seqs = list(range(600))
+    z = torch.zeros((600 * 2144, 1, D), dtype=torch.bfloat16, device="cuda")
+    p.c.extend(ints(seqs), offsets([2144] * 600))
+    assert p.m.extend(seqs, [2144] * 600) is False       # 40200 pages are more than there are
+    import paper_2505_13109_amd as fkv
+    with pytest.raises(fkv.FreeKVError, match="too few free pages"):
+        p.c.health()
+    p.check_tables()
+    p.c.extend(ints(seqs), offsets([2100] * 600))
+    assert p.m.extend(seqs, [2100] * 600)
+    p.check_tables()
+    p.c.append(0, ints(seqs), z[:600 * 2100], z[:600 * 2100], offsets([2100] * 600))
+    p.c.free(ints(seqs[::3]))
+    p.m.free(seqs[::3])
+    p.check_tables()
+    p.c.extend(ints(seqs[:300:3]), offsets([70] * 100))
+    assert p.m.extend(seqs[:300:3], [70] * 100)
+    p.check_tables()
+    p.c.compact()
+    p.m.compact()
+    p.check_tables()
+
+
+# ---- what the device refuses ------------------------------------------------------------------------------
+
+def _refused(p, match):
+    import paper_2505_13109_amd as fkv
+    with pytest.raises(fkv.FreeKVError, match=match):
+        p.c.health()
+    p.c.health()                                         # reported once
+
+
+def test_refusals_change_nothing():
+    p = Pair(n_layers=2, n_kv=2, max_seqs=4, max_ctx=128, n_pages=4)
+    p.grow([0, 1], [70, 40])
+    # too few pages: nobody grows, and what they would have stored is dropped
+    k = torch.full((51, 2, D), 5.0, dtype=torch.bfloat16, device="cuda")
+    p.c.extend(ints([0, 1]), offsets([26, 25]))
+    p.c.append(0, ints([0, 1]), k, k, offsets([26, 25]))
+    _refused(p, "too few free pages")
+    p.check_tables()
+    p.check_contents()
+    # past max_ctx: that row stays, the others grow
+    p.c.free(ints([1]))
+    p.m.free([1])
+    p.c.extend(ints([0, 2]), offsets([59, 3]))
+    assert p.m.extend([2], [3])
+    for layer in range(2):
+        kk, vv = tokens(p.gen, 62, 2, "bf16")
+        p.c.append(layer, ints([0, 2]), kk.cuda(), vv.cuda(), offsets([59, 3]))
+        p.m.append(layer, [2], [3], kk[59:], vv[59:])
+    _refused(p, "max_ctx")
+    p.check_tables()
+    p.check_contents()
+    # slots that do not exist, and one named twice: the others go on
+    p.c.extend(ints([4, -2, 2, 2]))
+    assert p.m.extend([2], [1])
+    kk, vv = tokens(p.gen, 4, 2, "bf16")
+    for layer in range(2):
+        p.c.append(layer, ints([4, -2, 2, 2]), kk.cuda(), vv.cuda())
+        p.m.append(layer, [2], [1], kk[2:3], vv[2:3])
+    _refused(p, "passed over")
+    p.check_tables()
+    p.check_contents()
+    # a fork onto a sequence, onto one slot twice, from and to nowhere
+    p.c.fork(ints([0, 0, 0, 9]), ints([2, 1, 1, 3]))
+    p.m.fork([0], [1])
+    p.c.fork(ints([0]), ints([77]))
+    _refused(p, "passed over")
+    p.check_tables()
+    # freed twice in one call: once
+    p.c.free(ints([1, 1, 8]))
+    p.m.free([1])
+    _refused(p, "passed over")
+    p.check_tables()
+    p.c.copy(ints([0, 2]), ints([1, 3]))                 # two full pages are needed; two are free
+    assert p.m.copy([0, 2], [1, 3])
+    p.c.health()
+    p.check_tables()
+    p.c.free(ints([3]))
+    p.m.free([3])
+    p.c.copy(ints([0]), ints([3]))
+    assert not p.m.copy([0], [3])
+    _refused(p, "too few free pages")
+    p.check_tables()
+    p.check_contents()
+    q = p.queries(3)
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    p.c.attn(0, ints([9, -1, 3]), q.cuda(), out)
+    assert not out.any()
+    _refused(p, "passed over")
+
+
+def test_a_fork_of_an_empty_slot_that_another_entry_fills_stays_empty():
+    p = Pair(n_kv=1, max_seqs=4)
+    p.grow([0], [70])
+    p.c.fork(ints([0, 1]), ints([1, 2]))                 # slot 1 is empty when the call begins
+    p.m.fork([0], [1])
+    p.check_tables()
+    p.c.free(ints([0, 1]))
+    p.m.free([0, 1])
+    p.check_tables()
+    assert p.c.used_pages() == 0
+
+
+def test_tokens_come_once_per_layer_and_extend():
+    p = Pair(n_layers=2, n_kv=1, max_seqs=3)
+    for n in (3, 40, 100):
+        p.grow([0, 1], [n, 5])
+        other = torch.full((n + 5, 1, D), 9.0, dtype=torch.bfloat16, device="cuda")
+        p.c.append(1, ints([0, 1]), other, other, offsets([n, 5]))        # a second time
+        _refused(p, "passed over")
+        p.c.append(1, ints([1, 0]), other, other, offsets([5, n]))        # in other rows
+        _refused(p, "passed over")
+        p.check_contents()
+    p.c.append(1, ints([2]), other[:1], other[:1])       # never extended
+    _refused(p, "passed over")
+    p.c.extend(ints([0, 1]), offsets([4, 4]))
+    assert p.m.extend([0, 1], [4, 4])
+    k, v = tokens(p.gen, 8, 1, "bf16")
+    p.c.append(0, ints([0, 1]), k.cuda(), v.cuda(), offsets([3, 5]))      # other numbers of tokens
+    _refused(p, "passed over")
+    for layer in range(2):
+        p.c.append(layer, ints([0, 1]), k.cuda(), v.cuda(), offsets([4, 4]))
+        p.m.append(layer, [0, 1], [4, 4], k, v)
+    p.check_contents()
+    p.check_tables()
+
+
+def test_token_offsets_that_make_no_sense_reach_nothing():
+    """Offsets past the tokens that are there, falling, negative: rows are dropped, nothing is read or written for them."""
+    p = Pair(n_kv=1, max_seqs=4, max_ctx=256, n_pages=32)
+    p.grow([0], [40])
+    k, v = tokens(p.gen, 8, 1, "bf16")
+    for cu in ([0, 8, 4], [0, 100, 108], [-50, 4, 8], [64, 68, 70], [8, 0, 2 ** 31 - 1]):
+        p.c.append(0, ints([0, 1]), k.cuda(), v.cuda(), ints(cu))
+        shape = (8, 1, D)
+        a, b = (torch.zeros(shape, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+        p.c.read(0, ints([0, 1]), a, b, ints(cu))
+    import paper_2505_13109_amd as fkv
+    with pytest.raises(fkv.FreeKVError):
+        p.c.health()
+    p.check_tables()
+    p.check_contents()
+
+
+def test_arguments_are_refused_before_a_launch():
+    import paper_2505_13109_amd as fkv
+    p = Pair(n_kv=2, G=2, max_seqs=4)
+    c, q = p.c, p.queries(2).cuda()
+    k = torch.zeros((2, 2, D), dtype=torch.bfloat16, device="cuda")
+    s = ints([0, 1])
+    bad = [
+        lambda: c.attn(1, s, q, q.clone()),                                       # layer
+        lambda: c.attn(0, s, q.float(), q.clone()), lambda: c.attn(0, s, q[:1], q.clone()),
+        lambda: c.attn(0, s, q.cpu(), q.clone()), lambda: c.attn(0, s, q, q.clone(), sink=32),
+        lambda: c.attn(0, s, q, q.clone(), pages=torch.zeros((2, 2, 3), dtype=torch.int64, device="cuda")),
+        lambda: c.attn(0, s, q, q.clone(), pages=torch.zeros((2, 2, 3), dtype=torch.int32, device="cuda"), sink=20),
+        lambda: c.attn(0, s, q, q.clone(), pages=torch.zeros((2, 2, 17), dtype=torch.int32, device="cuda")),
+        lambda: c.attn(0, s.long(), q, q.clone()), lambda: c.extend(ints([0] * 5)), lambda: c.extend(s, ints([0, 1])),
+        lambda: c.append(0, s, k[:1], k[:1]), lambda: c.append(0, s, k, k[:1]), lambda: c.append(0, s, k.half(), k),
+        lambda: c.append(0, s, k.transpose(0, 1), k), lambda: c.append(-1, s, k, k), lambda: c.read(0, s, k[..., :64], k),
+        lambda: c.fork(s, ints([1])), lambda: c.tables(s, s, s),
+        lambda: c.append(0, s, torch.zeros(2 * 2 * D + 4, dtype=torch.bfloat16, device="cuda")[4:].view(2, 2, D), k),      # 8-byte aligned
+        lambda: c.copy(s, s, to=Pair(n_kv=1, G=2).c),
+    ]
+    for call in bad:
+        with pytest.raises(fkv.FreeKVError):
+            call()
+    none = ints([])
+    c.extend(none), c.free(none), c.fork(none, none)
+    c.append(0, none, k[:0], k[:0]), c.attn(0, none, q[:0], q[:0])
+    p.check_tables()
+
+
+# ---- graphs and streams --------------------------------------------------------------------------------------
+
+def test_a_captured_step_goes_on_with_every_replay():
+    """extend, append and attention of two layers in one graph: each replay appends the tokens its inputs hold by then.  Between the
+    replays the program goes on by itself: branches, an eager step, a compaction."""
+    p = Pair(n_layers=2, n_kv=2, G=4, max_seqs=4, max_ctx=512, n_pages=64)
+    p.grow([0, 1, 2], [60, 5, 31])
+    seqs = ints([0, 2, -1])
+    kv = [[torch.zeros((3, 2, D), dtype=torch.bfloat16, device="cuda") for _ in "kv"] for _ in range(2)]
+    q = torch.zeros((3, 8, D), dtype=torch.bfloat16, device="cuda")
+    out = [torch.zeros_like(q) for _ in range(2)]
+
+    def step():
+        p.c.extend(seqs)
+        for layer in range(2):
+            p.c.append(layer, seqs, *kv[layer])
+            p.c.attn(layer, seqs, q, out[layer])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for i in range(40):
+        rows = [0, 2]
+        new = [tokens(p.gen, 3, 2, "bf16") for _ in range(2)]
+        for layer in range(2):
+            for a, b in zip(kv[layer], new[layer]):
+                a.copy_(b)
+        qq = p.queries(3)
+        q.copy_(qq)
+        graph.replay()
+        assert p.m.extend(rows, [1, 1])
+        for layer in range(2):
+            p.m.append(layer, rows, [1, 1], new[layer][0], new[layer][1])
+            if i % 7 == 0 or p.m.len[0] % 32 < 2:
+                p.check_attention(layer, [0, 2, -1], q=qq, got=out[layer].cpu())
+        if i == 10:
+            p.grow([1, 0], [40, 3])
+        if i == 20:
+            p.c.free(ints([1]))
+            p.m.free([1])
+            p.c.compact()
+            p.m.compact()
+        if i == 25:
+            p.c.fork(ints([0]), ints([3]))
+            p.m.fork([0], [3])
+    p.check_tables()
+    p.check_contents()
+
+
+def test_branches_in_a_graph():
+    """fork, extend, append, attention, free: every replay begins where the last one began."""
+    p = Pair(n_layers=1, n_kv=2, G=2, max_seqs=6, max_ctx=256, n_pages=40)
+    p.grow([0], [95])
+    src, dst = ints([0, 0, 0]), ints([1, 2, 3])
+    k, v = (t.cuda() for t in tokens(p.gen, 3, 2, "bf16"))
+    q = p.queries(3).cuda()
+    out, lens, pages = torch.zeros_like(q), ints([0] * 3), torch.zeros((3, 8), dtype=torch.int32, device="cuda")
+
+    def step():
+        p.c.fork(src, dst)
+        p.c.extend(dst)
+        p.c.append(0, dst, k, v)
+        p.c.attn(0, dst, q, out)
+        p.c.tables(dst, lens, pages)
+        p.c.free(dst)
+
+    step()
+    want = out.clone(), lens.clone(), pages.clone()
+    assert lens.tolist() == [96] * 3 and pages[:, 2].tolist() == [2, 3, 4]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(5):
+        out.zero_(), lens.zero_(), pages.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lens, want[1]) and torch.equal(pages, want[2])
+        p.check_tables()
+
+
+def test_on_a_stream_of_the_callers():
+    p = Pair(n_kv=2, G=2, max_seqs=2)
+    s = torch.cuda.Stream()
+    k, v = tokens(p.gen, 70, 2, "bf16")
+    kd, vd, q = k.cuda(), v.cuda(), p.queries(1)
+    qd, seqs, cu = q.cuda(), ints([1]), offsets([70])
+    out = torch.zeros_like(qd)
+    s.wait_stream(torch.cuda.current_stream())
+    p.c.extend(seqs, cu, stream=s)
+    p.c.append(0, seqs, kd, vd, cu, stream=s)
+    p.c.attn(0, seqs, qd, out, stream=s)
+    s.synchronize()
+    assert p.m.extend([1], [70])
+    p.m.append(0, [1], [70], k, v)
+    p.check_attention(0, [1], q=q, got=out.cpu())
+
+
+def test_two_caches_at_once_on_two_streams():
+    a, b = (Pair(n_kv=2, G=4, max_seqs=2, max_ctx=8192, n_pages=300, seed=i) for i in (1, 2))
+    for p in (a, b):
+        p.grow([0], [8000])
+    torch.cuda.synchronize()
+    streams, qs = [torch.cuda.Stream() for _ in "ab"], [p.queries(1) for p in (a, b)]
+    qd = [q.cuda() for q in qs]
+    outs = [[torch.zeros_like(q) for _ in range(20)] for q in qd]
+    seqs = ints([0])
+    torch.cuda.synchronize()
+    for i in range(20):
+        for p, s, q, o in zip((a, b), streams, qd, outs):
+            p.c.attn(0, seqs, q, o[i], stream=s)
+    torch.cuda.synchronize()
+    for p, q, o in zip((a, b), qs, outs):
+        p.check_attention(0, [0], q=q, got=o[0].cpu())
+        assert all(torch.equal(o[0], x) for x in o[1:])
