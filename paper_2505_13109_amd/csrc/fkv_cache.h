@@ -33,7 +33,7 @@ enum { CACHE_USED = 0, CACHE_FAULTS = 1, CACHE_MOVES = 2, CACHE_HEAD = 64 };
 enum { FAULT_PAGES = 1, FAULT_RANGE = 2, FAULT_ENTRY = 4 };
 
 constexpr int CACHE_MAX_SEQS = 4096;
-constexpr int CACHE_MAX_SPLITS = 256;
+constexpr int CACHE_MAX_SPLITS = 256, CACHE_TICKETS = 33;
 constexpr int CACHE_MAX_G = 16;
 
 struct CacheDesc {
@@ -53,16 +53,17 @@ struct CacheDesc {
   int32_t* to;           //        to page
   int32_t* remap;        // [page] new number of a page that moved
   int32_t* ok;           // [slot] fork, copy: the source of entry i, -1: nothing to do
-  float* part;           // attention: partial sums of a split, [item][G][d], and
-  float* part_ml;        // [item][G] maxima, [item][G] sums
-  int32_t* ticket;       // [row][n_kv] splits that are done
+  unsigned long long* part;      // attention: a split's sums, pairs of channels, [item][n_kv][G][d / 2], and
+  unsigned long long* part_ml;   // [item][n_kv][G] its maximum and sum of weights
+  unsigned long long* group_ml;  // the same of a group of splits, at its first one
+  int32_t* ticket;       // [row][n_kv][CACHE_TICKETS] splits that are done: of all groups, and of each group
   int n_layers, n_kv, G, max_seqs, max_pages, n_pages, dtype;
 
   __host__ __device__ size_t unit(int layer, int page, int m) const { return ((size_t)layer * n_pages + page) * n_kv + m; }
   __host__ __device__ size_t open_at(int layer, int slot, int m) const { return (((size_t)layer * max_seqs + slot) * n_kv + m) * OPEN_ELEMS; }
 };
 
-// Blocks that attention is cut into, about: see attn_cache_kernel.
+// Blocks that attention is cut into, about: two of four waves for each of 256 compute units.
 constexpr int CACHE_ATTN_BLOCKS = 512;
 inline int cache_attn_items(int n_rows, int n_kv) { return CACHE_ATTN_BLOCKS / n_kv + n_rows + 1; }
 

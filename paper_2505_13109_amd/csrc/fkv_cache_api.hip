@@ -51,13 +51,14 @@ size_t lay_out(const fkv_cache_config& c, char* base, CacheDesc* d) {
   take(x.appended, opens * 4);
   take(x.ref, (size_t)c.n_pages * 4);
   take(x.used, (size_t)(c.n_pages + 31) / 32 * 4);
-  take(x.ticket, (size_t)c.max_seqs * c.n_kv_heads * 4);
+  take(x.ticket, (size_t)c.max_seqs * c.n_kv_heads * CACHE_TICKETS * 4);
   take(x.table, (size_t)c.max_seqs * x.max_pages * 4);
   take(x.from, (size_t)c.n_pages * 4);
   take(x.to, (size_t)c.n_pages * 4);
   take(x.remap, (size_t)c.n_pages * 4);
   take(x.ok, (size_t)c.max_seqs * 4);
-  take(x.part_ml, items * x.G * 2 * 4);
+  take(x.part_ml, items * x.G * 8);
+  take(x.group_ml, items * x.G * 8);
   take(x.part, items * x.G * D * 4);
   take(x.exps, units * 4);
   take(x.open, opens * OPEN_ELEMS * 2);

@@ -27,27 +27,33 @@ __device__ __forceinline__ half8 codes_of(uint32_t w) {
 }
 __device__ __forceinline__ half8 ones_of() { return codes_of(0x11111111u); }
 
-// One page of one KV head, as a lane has it.
-struct PageRegs {
-  uint4 k[2], v[2], kstep[4], klo[4], vstep, vlo;
+// The halves of a page of one KV head, as a lane has them.
+struct Keys {
+  uint4 k[2], step[4], lo[4];
   int exps;
 };
-__device__ __forceinline__ void load_page(const CacheDesc& c, size_t u, int lane, PageRegs& r) {
+struct Values {
+  uint4 v[2], step, lo;
+};
+__device__ __forceinline__ void load_keys(const CacheDesc& c, size_t u, int lane, Keys& r) {
   const uint16_t* const unit = reinterpret_cast<const uint16_t*>(c.units + u * CU_BYTES);
-  const int kb = lane >> 4, n = lane & 15;
+  const int kb = lane >> 4;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    r.k[i] = load_past(unit + CU_K / 2 + i * 512 + lane * 8);
-    r.v[i] = load_past(unit + CU_V / 2 + i * 512 + lane * 8);
-  }
+  for (int i = 0; i < 2; ++i) r.k[i] = load_past(unit + CU_K / 2 + i * 512 + lane * 8);
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
-    r.kstep[s] = load_past(unit + CU_KSTEP / 2 + kb * 32 + s * 8);
-    r.klo[s] = load_past(unit + CU_KLO / 2 + kb * 32 + s * 8);
+    r.step[s] = load_past(unit + CU_KSTEP / 2 + kb * 32 + s * 8);
+    r.lo[s] = load_past(unit + CU_KLO / 2 + kb * 32 + s * 8);
   }
-  r.vstep = load_past(unit + CU_VSTEP / 2 + n * 8);
-  r.vlo = load_past(unit + CU_VLO / 2 + n * 8);
   r.exps = c.exps[u];
+}
+__device__ __forceinline__ void load_values(const CacheDesc& c, size_t u, int lane, Values& r) {
+  const uint16_t* const unit = reinterpret_cast<const uint16_t*>(c.units + u * CU_BYTES);
+  const int n = lane & 15;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) r.v[i] = load_past(unit + CU_V / 2 + i * 512 + lane * 8);
+  r.step = load_past(unit + CU_VSTEP / 2 + n * 8);
+  r.lo = load_past(unit + CU_VLO / 2 + n * 8);
 }
 
 // What a wave has seen of a row.  Lane (kb, n): query head n where tokens or channels are the other index of a product, heads
@@ -59,10 +65,17 @@ struct Seen {
   f32x4 l, acc[8];                   // of head 4 kb + i; channels cb 16 + n
 };
 
+// max over the lanes n, n + 16, n + 32, n + 48
+__device__ __forceinline__ float max_groups(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // The maximum moves up where a weight would otherwise pass the headroom: for most pages it does not.
 __device__ __forceinline__ void raise(Seen& s, float top, int lane) {
-  top = fmaxf(top, __shfl_xor(top, 16));
-  top = fmaxf(top, __shfl_xor(top, 32));
+  top = max_groups(top);
   if (!__any(top > s.m + LAG)) return;
   const float m = fmaxf(s.m, top), f = exp2f(s.m - m);
   s.m = m;
@@ -74,15 +87,15 @@ __device__ __forceinline__ void raise(Seen& s, float top, int lane) {
   for (int cb = 0; cb < 8; ++cb) s.acc[cb] *= g;
 }
 
-// A full page.  x = q (lo + step code): the product of q and step is made here, per page and channel, in two fp16 halves
-// (exact: 8 or 11 bits times 11); the codes are the other operand.  v likewise: the weights times the codes, and step and
-// lo of a channel are applied to the page's sums.
+// A full page's keys: x = q (lo + step code).  The product of q and step is made here, per page and channel, in two fp16 halves
+// (exact: 8 or 11 bits times 11); the codes are the other operand.  x[mb][i]: head n, token mb 16 + kb 4 + i, in powers of two.
 template <int DT>
-__device__ __forceinline__ void full_page(const PageRegs& r, const half8* q16, const u32x4* qT, int q_exp, float scale, int lane, Seen& s) {
-  f32x4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, bias = {0, 0, 0, 0};
+__device__ __forceinline__ void page_logits(const Keys& r, const half8* q16, const u32x4* qT, int q_exp, float scale, f32x4* x) {
+  f32x4 bias = {0, 0, 0, 0};
+  x[0] = x[1] = bias;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const half8 step = __builtin_bit_cast(half8, r.kstep[j]);
+    const half8 step = __builtin_bit_cast(half8, r.step[j]);
     const half8 hi = q16[j] * step;
     const half8 lo = __builtin_elementwise_fma(q16[j], step, -hi);
     const uint32_t w0 = j == 0 ? r.k[0].x : j == 1 ? r.k[0].y : j == 2 ? r.k[0].z : r.k[0].w;
@@ -92,29 +105,41 @@ __device__ __forceinline__ void full_page(const PageRegs& r, const half8* q16, c
     x[1] = mfma_h(a1, hi, x[1]);
     x[0] = mfma_h(a0, lo, x[0]);
     x[1] = mfma_h(a1, lo, x[1]);
-    bias = mfma_T<DT>(__builtin_bit_cast(u32x4, r.klo[j]), qT[j], bias);
+    bias = mfma_T<DT>(__builtin_bit_cast(u32x4, r.lo[j]), qT[j], bias);
   }
   const int e = min(max((int)(int16_t)(r.exps & 0xffff) + q_exp, -140), 126);
   const float f = ldexpf(scale, e), b = bias[0] * scale;
-  float top = -INFINITY;
 #pragma unroll
   for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[mb][i] = fmaf(x[mb][i], f, b);
-      top = fmaxf(top, x[mb][i]);
-    }
-  raise(s, top, lane);
-  const float off0 = s.m - HEADROOM, off2 = off0 + 4.f;
+    for (int i = 0; i < 4; ++i) x[mb][i] = fmaf(x[mb][i], f, b);
+}
+
+__device__ __forceinline__ float max8(const f32x4* x) {
+  float top = x[0][0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j >> 2][j & 3]);
+  return top;
+}
+
+// Its weights, with what the codes of the other operand want of them: 2^-4 where those are 2^4 larger.
+__device__ __forceinline__ half8 page_weights(const f32x4* x, float m) {
+  const float off0 = m - HEADROOM, off2 = off0 + 4.f;
   half8 p;
 #pragma unroll
   for (int j = 0; j < 8; ++j) p[j] = (_Float16)__builtin_amdgcn_exp2f(x[j >> 2][j & 3] - ((j & 2) ? off2 : off0));
+  return p;
+}
+
+// Its values: the weights times the codes, and step and lo of a channel are applied to the page's sums.
+template <int DT>
+__device__ __forceinline__ void page_sums(const Values& r, int exps, half8 p, Seen& s) {
   const f32x4 none = {0, 0, 0, 0};
   const f32x4 sum = mfma_h(p, ones_of(), none);
   s.l += sum;
-  const half8 vstep = __builtin_bit_cast(half8, r.vstep);
-  const float vscale = ldexpf(1.f, r.exps >> 16);
-  const uint32_t lo2[4] = {r.vlo.x, r.vlo.y, r.vlo.z, r.vlo.w};
+  const half8 vstep = __builtin_bit_cast(half8, r.step);
+  const float vscale = ldexpf(1.f, exps >> 16);
+  const uint32_t lo2[4] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w};
   const uint32_t vw[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) {
@@ -178,6 +203,12 @@ __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const 
   }
 }
 
+// 256 blocks of eight waves take as long (32K tokens 14.6 us against 14.5, 128K x 4 118 against 120) but leave ragged batches less to
+// balance with (33 against 27); three waves to a SIMD, 168 registers, 17.7 and 135.
+constexpr int WAVES = 4, THREADS = WAVES * 64;
+// Splits that are joined at once, and how many there may be for one level of that.  By 16: 17.3 us for 32K tokens, by 32: 18.1.
+constexpr int JOIN = 8, ONE_LEVEL = 12;
+
 // How a row's attention is cut: positions are the pages to attend in order (sink, list, window, or all), the open page last.
 struct Cut {
   int len, full, sink, win, listed, positions;
@@ -196,99 +227,230 @@ struct Cut {
     positions = sink + listed + win + (len % PG ? 1 : 0);
   }
 };
+__device__ __forceinline__ int chunk_for(int total, int parts) { return max(2 * WAVES, (int)((uint32_t)(total + parts - 1) / (uint32_t)parts)); }
 // Splits of a row of `positions` where a split has `chunk`, at most CACHE_MAX_SPLITS.
 __device__ __forceinline__ int splits_of(int positions, int chunk) {
-  return max(1, min((positions + chunk - 1) / chunk, CACHE_MAX_SPLITS));
+  return max(1, min((int)((uint32_t)(positions + chunk - 1) / (uint32_t)chunk), CACHE_MAX_SPLITS));
+}
+// sums over the lanes up to this one
+__device__ __forceinline__ int scan_wave(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr:1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // a row's last lane into the next row, then into the other half
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
+// The row and split that are a launch's item-th.  positions(r0): this lane's row r0 + lane's, 0 behind the last row.
+//
+// There is room for CACHE_ATTN_BLOCKS blocks at once, so for `room` splits of all rows together.  Rows are cut into equal chunks: of a
+// few sizes, from the one that lengths without remainders would allow to the one that any lengths do, the smallest that leaves no
+// split for a second round (32 requests of 500 to 16K tokens, 28/4 heads: 30 us; with about as many splits as there is room
+// 34).  Where there are more rows than half the room, about as many splits as there is room.
+struct Place {
+  int row, split, n_splits;
+};
+template <typename F>
+__device__ __forceinline__ Place place_of(int item, int n_rows, int n_kv, int lane, F positions) {
+  const int room = max(CACHE_ATTN_BLOCKS / n_kv, 1);
+  int total = 0;
+  for (int r0 = 0; r0 < n_rows; r0 += 64) total += (int)wave_sum_u32((uint32_t)positions(r0));
+  int chunk = chunk_for(total, room);
+  if (n_rows <= room / 2) {
+    constexpr int TRIES = 4;
+    const int back[TRIES] = {0, (n_rows + 3) / 4, (n_rows + 1) / 2, n_rows};
+    int sum[TRIES] = {0, 0, 0, 0}, size[TRIES];
+#pragma unroll
+    for (int t = 0; t < TRIES; ++t) size[t] = chunk_for(total, room - back[t]);
+    for (int r0 = 0; r0 < n_rows; r0 += 64) {
+      const int p = positions(r0);
+#pragma unroll
+      for (int t = 0; t < TRIES; ++t) sum[t] += r0 + lane < n_rows ? splits_of(p, size[t]) : 0;
+    }
+    chunk = size[TRIES - 1];
+#pragma unroll
+    for (int t = TRIES - 2; t >= 0; --t)
+      if ((int)wave_sum_u32((uint32_t)sum[t]) <= room) chunk = size[t];
+  }
+  Place at = {-1, 0, 0};
+  int before = 0;
+  for (int r0 = 0; r0 < n_rows; r0 += 64) {
+    const int k = r0 + lane < n_rows ? splits_of(positions(r0), chunk) : 0, upto = before + scan_wave(k);
+    const unsigned long long here = __ballot(item < upto);
+    if (here) {
+      const int i = __ffsll((long long)here) - 1;
+      at.row = r0 + i;
+      at.n_splits = __builtin_amdgcn_readlane(k, i);
+      at.split = item - (__builtin_amdgcn_readlane(upto, i) - at.n_splits);
+      break;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  return at;
+}
+
+// Values that blocks of one launch hand each other: at device scope, past the caches of one XCD.  A fence would write back all that
+// its L2 holds (28 us of 52 for 32K tokens, 70 of 202 for four times 128K); these stores are in memory when they count as done.
+__device__ __forceinline__ void hand_on(unsigned long long* p, float a, float b) {
+  __hip_atomic_store(p, (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long take_over(const unsigned long long* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float first_of(unsigned long long w) { return __uint_as_float((uint32_t)w); }
+__device__ __forceinline__ float second_of(unsigned long long w) { return __uint_as_float((uint32_t)(w >> 32)); }
+
+// Joins what `count` splits have of N pairs of channels, THREADS pairs apart: a maximum m and sums x, y and l each.
+struct Joined {
+  float m, l, x, y;
+};
+template <int N>
+__device__ __forceinline__ void join(const unsigned long long* part, const unsigned long long* ml, size_t part_step, size_t ml_step, int count, Joined* r) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) r[j] = Joined{-1e30f, 0.f, 0.f, 0.f};
+  for (int k0 = 0; k0 < count; k0 += JOIN) {
+    unsigned long long v[N][JOIN], w[N][JOIN];
+#pragma unroll
+    for (int k = 0; k < JOIN; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const size_t at = (size_t)min(k0 + k, count - 1);
+        w[j][k] = take_over(ml + at * ml_step + j * (THREADS / (D / 2)));
+        v[j][k] = take_over(part + at * part_step + j * THREADS);
+      }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      float m = r[j].m;
+#pragma unroll
+      for (int k = 0; k < JOIN; ++k) m = fmaxf(m, first_of(w[j][k]));      // (the last one again, where there are fewer)
+      const float f0 = __builtin_amdgcn_exp2f(r[j].m - m);
+      r[j].m = m; r[j].l *= f0; r[j].x *= f0; r[j].y *= f0;
+#pragma unroll
+      for (int k = 0; k < JOIN; ++k)
+        if (k0 + k < count) {
+          const float f = __builtin_amdgcn_exp2f(first_of(w[j][k]) - m);
+          r[j].l = fmaf(f, second_of(w[j][k]), r[j].l);
+          r[j].x = fmaf(f, first_of(v[j][k]), r[j].x);
+          r[j].y = fmaf(f, second_of(v[j][k]), r[j].y);
+        }
+    }
+  }
+}
+// All of a head's pairs, a thread's one or two at a time; got(pair, joined).
+template <typename F>
+__device__ __forceinline__ void join_all(const unsigned long long* part, const unsigned long long* ml, size_t part_step, size_t ml_step, int count, int pairs,
+                                         F got) {
+  Joined r[2];
+  int i = threadIdx.x;
+  for (; i + THREADS < pairs; i += 2 * THREADS) {
+    join<2>(part + i, ml + i / (D / 2), part_step, ml_step, count, r);
+    got(i, r[0]);
+    got(i + THREADS, r[1]);
+  }
+  if (i < pairs) {
+    join<1>(part + i, ml + i / (D / 2), part_step, ml_step, count, r);
+    got(i, r[0]);
+  }
+}
+template <int DT> __device__ __forceinline__ uint32_t quotients(float x, float y, float l) {
+  return to_T<DT>(l == 0.f ? 0.f : x / l) | (uint32_t)to_T<DT>(l == 0.f ? 0.f : y / l) << 16;
 }
 
 // A block per (split of a row, KV head), the heads of a split next to each other.  Rows are cut into equal chunks, so that about
 // CACHE_ATTN_BLOCKS blocks have something to do whatever the lengths are: every block works out the cut from the lengths,
-// which only the device knows.  A block's four waves take positions in turn, each with its own maximum and sums; they are
+// which only the device knows.  A block's waves take positions in turn, each with its own maximum and sums; they are
 // joined in LDS, and the splits of a row by the block that finishes last.
 template <int DT>
-__global__ __launch_bounds__(256, 2) void attn_cache_kernel(CacheDesc c, CacheAttn a) {
-  __shared__ float s_m[4][CACHE_MAX_G], s_l[4][CACHE_MAX_G];
-  __shared__ __attribute__((aligned(16))) float s_acc[4 * CACHE_MAX_G * D];
-  __shared__ int s_cut[8], s_sum[4];
+__global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, CacheAttn a) {
+  __shared__ float s_m[WAVES][CACHE_MAX_G], s_l[WAVES][CACHE_MAX_G];
+  __shared__ __attribute__((aligned(16))) float s_acc[WAVES * CACHE_MAX_G * D];
+  __shared__ int s_last;
+  static_assert(CACHE_MAX_SEQS <= WAVES * CACHE_MAX_G * D && CACHE_MAX_SPLITS <= JOIN * (CACHE_TICKETS - 1), "");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int item = blockIdx.x / c.n_kv, head = blockIdx.x % c.n_kv, kb = lane >> 4, n = lane & 15;
 
-  // -- this block's row and split
-  constexpr int MIN_CHUNK = 8;
-  const int per = (a.n_rows + 255) / 256;
-  int mine = 0;
-  for (int j = 0; j < per; ++j) {
-    const int r = tid * per + j;
-    int slot;
-    Cut cut;
-    if (r < a.n_rows) { cut.of(c, a, r, &slot); mine += cut.positions; }
-  }
-  for (int o = 32; o; o >>= 1) mine += __shfl_xor(mine, o);
-  if (lane == 0) s_sum[wave] = mine;
-  if (tid == 0) s_cut[0] = -1;
-  __syncthreads();
-  const long total = ((long)s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * c.n_kv;
-  const int chunk = max(MIN_CHUNK, (int)((total + CACHE_ATTN_BLOCKS - 1) / CACHE_ATTN_BLOCKS));
-  __syncthreads();
-  int splits = 0;
-  for (int j = 0; j < per; ++j) {
-    const int r = tid * per + j;
-    int slot;
-    Cut cut;
-    if (r < a.n_rows) { cut.of(c, a, r, &slot); splits += splits_of(cut.positions, chunk); }
-  }
-  int before = splits;
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(before, o);
-    if (lane >= o) before += y;
-  }
-  if (lane == 63) s_sum[wave] = before;
-  __syncthreads();
-  before -= splits;
-  for (int w = 0; w < wave; ++w) before += s_sum[w];
-  if (item >= before && item < before + splits) {
-    for (int j = 0; j < per; ++j) {
-      const int r = tid * per + j;
-      int slot;
-      Cut cut;
-      if (r >= a.n_rows) break;
-      cut.of(c, a, r, &slot);
-      const int k = splits_of(cut.positions, chunk);
-      if (item < before + k) {
-        s_cut[0] = r; s_cut[1] = item - before; s_cut[2] = k;
-        break;
-      }
-      before += k;
-    }
-  }
-  __syncthreads();
-  const int row = __builtin_amdgcn_readfirstlane(s_cut[0]), split = __builtin_amdgcn_readfirstlane(s_cut[1]);
-  const int n_splits = __builtin_amdgcn_readfirstlane(s_cut[2]);
-  if (row < 0) return;
+  // -- this block's row and split: every wave by itself up to 64 rows
+  int row = 0, split = item, n_splits, slot;
   Cut cut;
-  int slot;
-  cut.of(c, a, row, &slot);
+  if (a.n_rows == 1) {
+    cut.of(c, a, 0, &slot);
+    n_splits = splits_of(cut.positions, chunk_for(cut.positions, max(CACHE_ATTN_BLOCKS / c.n_kv, 1)));
+    if (item >= n_splits) return;
+  } else {
+    Place at;
+    if (a.n_rows <= 64) {
+      int mine = 0;
+      if (lane < a.n_rows) {
+        cut.of(c, a, lane, &slot);
+        mine = cut.positions;
+      }
+      at = place_of(item, a.n_rows, c.n_kv, lane, [&](int) { return mine; });
+    } else {
+      int* const s_pos = reinterpret_cast<int*>(s_acc);
+      for (int r = tid; r < a.n_rows; r += THREADS) {
+        cut.of(c, a, r, &slot);
+        s_pos[r] = cut.positions;
+      }
+      __syncthreads();
+      at = place_of(item, a.n_rows, c.n_kv, lane, [&](int r0) { return r0 + lane < a.n_rows ? s_pos[r0 + lane] : 0; });
+    }
+    row = at.row; split = at.split; n_splits = at.n_splits;
+    if (row < 0) return;
+    cut.of(c, a, row, &slot);
+  }
   if (slot < 0 && head == 0 && tid == 0 && a.seqs[row] != -1) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
-  const int lo = (int)((long)cut.positions * split / n_splits), hi = (int)((long)cut.positions * (split + 1) / n_splits);
+  const int size = ((uint32_t)cut.positions + n_splits - 1) / (uint32_t)n_splits;
+  const int lo = split * size;
 
-  // -- the queries: lane (kb, n) has head n's channels 32 j + 8 kb + e, as they are and as fp16 numbers next to 2^13 that
-  //    carry the codes' weights
+  // -- the queries: lane (kb, n) has head n's channels 32 j + 8 kb + e, as they are and, further down, as fp16 numbers next
+  //    to 2^13 that carry the codes' weights
   u32x4 qT[4] = {};
-  half8 q16[4] = {};
-  int q_exp = 0;
   if (n < c.G) {
     const uint16_t* const q = a.q + ((size_t)row * c.n_kv * c.G + (size_t)head * c.G + n) * D + kb * 8;
 #pragma unroll
     for (int j = 0; j < 4; ++j) qT[j] = *reinterpret_cast<const u32x4*>(q + j * 32);
   }
+  const float scale = 0.08838834764831845f * 1.4426950408889634f;      // 1 / sqrt(128), in powers of two
+  Seen seen;
+  seen.m = -1e30f;
+  seen.l = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int cb = 0; cb < 8; ++cb) seen.acc[cb] = f32x4{0, 0, 0, 0};
+
+  // -- the open page: the first wave's of the last split, before anything else takes up registers
+  const int rest = cut.len % PG, last_split = split == n_splits - 1;
+  const int hi = min(lo + size, cut.positions - (rest ? 1 : 0));
+  if (rest && last_split && wave == 0) open_page<DT>(c.open + c.open_at(a.layer, slot, head), rest, qT, scale, lane, seen);
+  const int turn = rest && last_split ? (wave + WAVES - 1) % WAVES : wave;      // (it is a page as others are)
+
+  const int32_t* const table = c.table + (size_t)max(slot, 0) * c.max_pages;
+  auto page_at = [&](int p0) {                             // of this lane's position among 64 of this wave's from p0 on; -1: none
+    const int pos = p0 + lane * WAVES;
+    if (pos >= hi) return -1;
+    int at = pos;                                          // position in the sequence
+    if (a.pages && pos >= cut.sink) {
+      if (pos < cut.sink + cut.listed) {
+        at = a.pages[((size_t)row * c.n_kv + head) * a.n_list + pos - cut.sink];
+        if (at < cut.sink || at >= cut.full - cut.win) return -1;
+      } else {
+        at = cut.full - cut.win + (pos - cut.sink - cut.listed);
+      }
+    }
+    return table[at];
+  };
+  int page = page_at(lo + turn);
+
+  half8 q16[4];
+  int q_exp;
   {
     float top = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(Unpack<DT>::lo(qT[j][i])), fabsf(Unpack<DT>::hi(qT[j][i]))));
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = max_groups(top);
     q_exp = top > 0.f && top < INFINITY ? max(ilogbf(top), -126) : 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -298,50 +460,48 @@ __global__ __launch_bounds__(256, 2) void attn_cache_kernel(CacheDesc c, CacheAt
         q16[j][2 * i] = (_Float16)ldexpf(Unpack<DT>::lo(qT[j][i]), e);
         q16[j][2 * i + 1] = (_Float16)ldexpf(Unpack<DT>::hi(qT[j][i]), e);
       }
+    q_exp += 24 - 13;
   }
-  const float scale = 0.08838834764831845f * 1.4426950408889634f;      // 1 / sqrt(128), in powers of two
 
   // -- the pages
-  Seen seen;
-  seen.m = -1e30f;
-  seen.l = f32x4{0, 0, 0, 0};
-#pragma unroll
-  for (int cb = 0; cb < 8; ++cb) seen.acc[cb] = f32x4{0, 0, 0, 0};
-  const int32_t* const table = c.table + (size_t)max(slot, 0) * c.max_pages;
-  for (int p0 = lo + wave; p0 < hi; p0 += 256) {
-    const int pos = p0 + lane * 4;
-    int page = -1;                                         // -1: nothing; -2: the open page
-    if (pos < hi) {
-      int at = pos;                                        // position in the sequence
-      if (a.pages && pos >= cut.sink) {
-        if (pos < cut.sink + cut.listed) {
-          at = a.pages[((size_t)row * c.n_kv + head) * a.n_list + pos - cut.sink];
-          if (at < cut.sink || at >= cut.full - cut.win) at = -1;
-        } else {
-          at = cut.full - cut.win + (pos - cut.sink - cut.listed);
-        }
-      }
-      page = at < 0 ? -1 : at < cut.full ? table[at] : -2;
-    }
-    if (__any(page == -2)) open_page<DT>(c.open + c.open_at(a.layer, slot, head), cut.len % PG, qT, scale, lane, seen);
+  for (int p0 = lo + turn; p0 < hi; p0 += 64 * WAVES) {
+    if (p0 > lo + turn) page = page_at(p0);
     unsigned long long todo = __ballot(page >= 0);
-    if (!todo) continue;
-    PageRegs now, next;
-    int i = __ffsll((long long)todo) - 1;
-    load_page(c, c.unit(a.layer, __builtin_amdgcn_readlane(page, i), head), lane, now);
-    while (todo) {
-      todo &= todo - 1;
-      if (todo) {
-        i = __ffsll((long long)todo) - 1;
-        load_page(c, c.unit(a.layer, __builtin_amdgcn_readlane(page, i), head), lane, next);
+    // A page's keys are asked for when those of the page before have been used, its values likewise: one half is on its way while the
+    // other is worked on.
+    if (todo) {
+      Keys keys;
+      Values values;
+      auto next = [&] {
+        const int i = __ffsll((long long)todo) - 1;
+        todo &= todo - 1;
+        return c.unit(a.layer, __builtin_amdgcn_readlane(page, i), head);
+      };
+      size_t u = next();
+      load_keys(c, u, lane, keys);
+      load_values(c, u, lane, values);
+      f32x4 x[2];
+      int exps;
+      while (todo) {
+        exps = keys.exps;
+        page_logits<DT>(keys, q16, qT, q_exp, scale, x);
+        u = next();
+        load_keys(c, u, lane, keys);
+        raise(seen, max8(x), lane);
+        page_sums<DT>(values, exps, page_weights(x, seen.m), seen);
+        load_values(c, u, lane, values);
       }
-      full_page<DT>(now, q16, qT, q_exp + 24 - 13, scale, lane, seen);
-      now = next;
+      // (the last page apart: a load that may or may not be under way would have to be waited for)
+      exps = keys.exps;
+      page_logits<DT>(keys, q16, qT, q_exp, scale, x);
+      raise(seen, max8(x), lane);
+      page_sums<DT>(values, exps, page_weights(x, seen.m), seen);
     }
   }
 
   // -- the waves' sums
   const int G = c.G;
+  __syncthreads();                                         // (s_acc held the rows' positions)
   if (lane < 16) s_m[wave][lane] = seen.m;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -352,71 +512,74 @@ __global__ __launch_bounds__(256, 2) void attn_cache_kernel(CacheDesc c, CacheAt
       for (int cb = 0; cb < 8; ++cb) s_acc[(wave * G + g) * D + cb * 16 + n] = seen.acc[cb][i];
   }
   __syncthreads();
-  uint16_t* const out = a.out + ((size_t)row * c.n_kv + head) * G * D;
+  const int pairs = G * (D / 2);
+  uint32_t* const out = reinterpret_cast<uint32_t*>(a.out) + ((size_t)row * c.n_kv + head) * pairs;
   const size_t slab = (size_t)item * c.n_kv + head;
-  for (int i = tid; i < G * D; i += 256) {
-    const int g = i / D;
-    const float m = fmaxf(fmaxf(s_m[0][g], s_m[1][g]), fmaxf(s_m[2][g], s_m[3][g]));
-    float sum = 0.f, l = 0.f;
+  for (int i = tid; i < pairs; i += THREADS) {
+    const int g = i / (D / 2);
+    float m = s_m[0][g];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = exp2f(s_m[w][g] - m);
-      sum = fmaf(f, s_acc[w * G * D + i], sum);
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, s_m[w][g]);
+    float x = 0.f, y = 0.f, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w][g] - m);
+      const float2 v = *reinterpret_cast<const float2*>(&s_acc[w * G * D + 2 * i]);
+      x = fmaf(f, v.x, x);
+      y = fmaf(f, v.y, y);
       l = fmaf(f, s_l[w][g], l);
     }
     if (n_splits == 1) {
-      out[i] = to_T<DT>(l == 0.f ? 0.f : sum / l);
+      out[i] = quotients<DT>(x, y, l);
     } else {
-      c.part[slab * G * D + i] = sum;
-      if (i % D == 0) {
-        c.part_ml[(slab * 2) * G + g] = m;
-        c.part_ml[(slab * 2 + 1) * G + g] = l;
-      }
+      hand_on(c.part + slab * pairs + i, x, y);
+      if (i % (D / 2) == 0) hand_on(c.part_ml + slab * G + g, m, l);
     }
   }
   if (n_splits == 1) return;
 
-  // -- the splits': the last block to get here joins them, in their order
-  __threadfence();
-  __syncthreads();
-  if (tid == 0) {
-    const int done = atomicAdd(&c.ticket[row * c.n_kv + head], 1);
-    s_cut[3] = done == n_splits - 1;
-    if (done == n_splits - 1) c.ticket[row * c.n_kv + head] = 0;
-  }
-  __syncthreads();
-  if (!s_cut[3]) return;
-  __threadfence();
-  const size_t slab0 = (size_t)(item - split) * c.n_kv + head;
-  float* const weight = s_acc;                             // [n_splits][G]
-  for (int g = wave; g < G; g += 4) {
-    float m = -1e30f, l = 0.f;
-    for (int k = lane; k < n_splits; k += 64) m = fmaxf(m, c.part_ml[((slab0 + (size_t)k * c.n_kv) * 2) * G + g]);
-    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    for (int k = lane; k < n_splits; k += 64) {
-      const float f = exp2f(c.part_ml[((slab0 + (size_t)k * c.n_kv) * 2) * G + g] - m);
-      weight[k * G + g] = f;
-      l = fmaf(f, c.part_ml[((slab0 + (size_t)k * c.n_kv) * 2 + 1) * G + g], l);
+  // -- the splits': the last block to get here joins them; where there are many, groups of JOIN first, each by the last of its
+  //    own, and then the groups: one block alone takes in some 20 bytes a ns, 64 splits 10 us.
+  auto last_of = [&](int32_t* ticket, int count) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wave's values are in memory
+    __syncthreads();
+    if (tid == 0) {
+      const bool last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == count - 1;
+      s_last = last;
+      if (last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
-    if (lane == 0) s_l[0][g] = l;
+    __syncthreads();
+    return s_last != 0;
+  };
+  int32_t* const ticket = c.ticket + ((size_t)row * c.n_kv + head) * CACHE_TICKETS;
+  const size_t part_step = (size_t)c.n_kv * pairs, ml_step = (size_t)c.n_kv * G;
+  const size_t slab0 = (size_t)(item - split) * c.n_kv + head;
+  const unsigned long long* ml = c.part_ml;
+  int count = n_splits, stride = 1;
+  if (n_splits > ONE_LEVEL) {
+    const int group = split / JOIN, first = group * JOIN, here = min(JOIN, n_splits - first);
+    if (!last_of(ticket + 1 + group, here)) return;
+    const size_t at = slab0 + (size_t)first * c.n_kv;
+    join_all(c.part + at * pairs, c.part_ml + at * G, part_step, ml_step, here, pairs, [&](int i, const Joined& r) {
+      // (over the group's first slab, of which this thread alone has read pair i; maxima and sums, which many read, apart)
+      hand_on(c.part + at * pairs + i, r.x, r.y);
+      if (i % (D / 2) == 0) hand_on(c.group_ml + at * G + i / (D / 2), r.m, r.l);
+    });
+    count = (n_splits + JOIN - 1) / JOIN;
+    stride = JOIN;
+    ml = c.group_ml;
   }
-  __syncthreads();
-  for (int i = tid; i < G * D; i += 256) {
-    const int g = i / D;
-    float sum = 0.f;
-    for (int k = 0; k < n_splits; ++k) sum = fmaf(weight[k * G + g], c.part[(slab0 + (size_t)k * c.n_kv) * G * D + i], sum);
-    const float l = s_l[0][g];
-    out[i] = to_T<DT>(l == 0.f ? 0.f : sum / l);
-  }
+  if (!last_of(ticket, count)) return;
+  join_all(c.part + slab0 * pairs, ml + slab0 * G, part_step * stride, ml_step * stride, count, pairs,
+           [&](int i, const Joined& r) { out[i] = quotients<DT>(r.x, r.y, r.l); });
 }
 
 }  // namespace
 
 void launch_cache_attn(const CacheDesc& c, const CacheAttn& a, hipStream_t st) {
   const int grid = cache_attn_items(a.n_rows, c.n_kv) * c.n_kv;
-  if (c.dtype == 0) attn_cache_kernel<0><<<grid, 256, 0, st>>>(c, a);
-  else attn_cache_kernel<1><<<grid, 256, 0, st>>>(c, a);
+  if (c.dtype == 0) attn_cache_kernel<0><<<grid, THREADS, 0, st>>>(c, a);
+  else attn_cache_kernel<1><<<grid, THREADS, 0, st>>>(c, a);
 }
 
 }  // namespace fkv

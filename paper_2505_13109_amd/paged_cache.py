@@ -36,6 +36,7 @@ class PagedCache:
             raise FreeKVError("no GPU: the cache's operators are HIP kernels")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.dev_bytes = need.value
         self.dev_arena = torch.empty(self.dev_bytes, dtype=torch.uint8, device=self.device)
         with torch.cuda.device(self.device):
@@ -49,23 +50,23 @@ class PagedCache:
             raise FreeKVError(f"{what}: {rc}: {self.L.fkv_cache_last_error(self._h).decode()}")
 
     def _stream(self, stream):
-        return torch._C._cuda_getCurrentRawStream(self.device.index) if stream is None else stream.cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
 
+    # (a decode step's calls are a few microseconds of GPU time each, so what is right is told with few attribute reads)
     def _tensor(self, t, what, dtype, shape):
-        if t.dtype != dtype or t.device != self.device or not t.is_contiguous() or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-            raise FreeKVError(f"{what}: a contiguous {dtype} tensor of shape {shape} on {self.device} is wanted, this is {t.dtype} {tuple(t.shape)} on {t.device}"
-                              + ("" if t.is_contiguous() else ", not contiguous"))
-        return t.data_ptr()
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self._index and t.is_contiguous():
+            return t.data_ptr()
+        raise FreeKVError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device} is wanted, this is {t.dtype} {tuple(t.shape)} on {t.device}"
+                          + ("" if t.is_contiguous() else ", not contiguous"))
 
     def _rows(self, seqs, cu=None, what="seqs"):
-        at = self._tensor(seqs, what, torch.int32, (None,))
-        n = seqs.shape[0]
+        n = seqs.shape[0] if seqs.dim() == 1 else -1
+        at = self._tensor(seqs, what, torch.int32, (n,))
         return at, n, None if cu is None else self._tensor(cu, "cu", torch.int32, (n + 1,))
 
     def _kv(self, k, v):
-        shape = (None, self.cfg.n_kv_heads, self.cfg.head_dim)
-        a = self._tensor(k, "k", self.torch_dtype, shape)
-        return a, self._tensor(v, "v", self.torch_dtype, tuple(k.shape)), k.shape[0]
+        shape = (k.shape[0] if k.dim() else 0, self.cfg.n_kv_heads, self.cfg.head_dim)
+        return self._tensor(k, "k", self.torch_dtype, shape), self._tensor(v, "v", self.torch_dtype, shape), shape[0]
 
     def close(self):
         if self._h:
