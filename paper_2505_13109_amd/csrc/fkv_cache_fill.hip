@@ -5,55 +5,80 @@ namespace fkv {
 
 namespace {
 
+typedef short short2v __attribute__((ext_vector_type(2)));
+
+// 16 bytes that are not read again soon
+__device__ __forceinline__ void store_past(uint16_t* p, uint4 v) { __builtin_nontemporal_store(__builtin_bit_cast(word4, v), reinterpret_cast<word4*>(p)); }
+
 constexpr int TILE = D + 8;        // elements of a token's row in LDS: rows begin four banks apart
 
 // 2^e, -126 <= e <= 127
 __device__ __forceinline__ float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// max over the 128 threads of this thread's half of a 256-thread block; the whole block calls it
-__device__ __forceinline__ float max_half(float v, float* sh) {
-  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
-  const int h = threadIdx.x >> 7 << 1;
-  return fmaxf(sh[h], sh[h + 1]);
+// Two values of T as whole numbers in the same order (and back: it is its own inverse).
+__device__ __forceinline__ uint32_t in_order(uint32_t w) {
+  const uint32_t sign = (uint32_t)__builtin_bit_cast(int, __builtin_bit_cast(short2v, w) >> 15);
+  return w ^ (sign & 0x7fff7fffu);
+}
+__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(short2v, a), __builtin_bit_cast(short2v, b)));
+}
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(short2v, a), __builtin_bit_cast(short2v, b)));
 }
 
-// One channel's 32 values to codes.  The code is the nearest to the exact quotient: in fp32 the quotient, at most 30, is off by less
-// than 1e-5, so only one within 1e-4 of the middle between two codes is looked at again in fp64 (and what overflowed).
+// A channel's codes.  The code is the nearest to the exact quotient: in fp32 the quotient, at most 30, is off by less than 1e-5
+// (three roundings), so only where one comes within 2e-5 of the middle between two codes, it is looked at again in fp64.
 struct Channel {
-  float lo, step, inv;
-  double step64;
-  __device__ __forceinline__ uint32_t code(float x) const {
-    if (step64 == 0.0) return 0;
-    const float t = (x - lo) * inv;
-    float r = rintf(t);
-    if (!(fabsf(t - r) < 0.4999f)) r = (float)fmin(rint(((double)x - (double)lo) / step64), 15.0);
-    return (uint32_t)fminf(fmaxf(r, 0.f), 15.f);
-  }
+  float lo, inv;                   // inv: 1 / step, 0 for a step of 0
 };
+constexpr float NEAR = 0.5f - 2e-5f;
+// the quotient, at most 15, and the code as a float; off: the furthest that a quotient has been from its code so far
+__device__ __forceinline__ float code_of(const Channel& q, float x, float& off) {
+  const float t = fminf((x - q.lo) * q.inv, 15.f);
+  const float r = rintf(t);
+  off = fmaxf(off, fabsf(t - r));
+  return r;
+}
+__device__ __forceinline__ float code_again(const Channel& q, int e, _Float16 step16, float x, float r, bool all) {
+  const float t = fminf((x - q.lo) * q.inv, 15.f);
+  if (step16 == (_Float16)0 || (!all && fabsf(t - r) < NEAR)) return r;
+  const double step = ldexp((double)(float)step16, e);
+  return (float)fmin(rint(((double)x - (double)q.lo) / step), 15.0);
+}
+// eight codes to a word, e = 0..7 at nibble_of(e): sums of sixteen bits are exact in fp32
+__device__ __forceinline__ uint32_t word_of(const float* r) {
+  const float a = fmaf(r[6], 4096.f, fmaf(r[4], 256.f, fmaf(r[2], 16.f, r[0])));
+  const float b = fmaf(r[7], 4096.f, fmaf(r[5], 256.f, fmaf(r[3], 16.f, r[1])));
+  return (uint32_t)a | (uint32_t)b << 16;
+}
 
 // A block per (page that a row's tokens fill, KV head); the first one of a row also keeps the tokens that fill none.
-// 256 threads: one per channel of K and of V.
+// The page is staged in LDS: 256 threads take pairs of channels for the smallest and largest values, channels for the steps, and words
+// of eight codes in the end.
 template <int DT>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int layer, const int32_t* __restrict__ seqs, int n_rows,
                                                            const int32_t* __restrict__ cu, const uint16_t* __restrict__ K,
                                                            const uint16_t* __restrict__ V, int n_tokens, bool mark) {
   __shared__ __attribute__((aligned(16))) uint16_t tile[2][PG][TILE];
-  __shared__ uint32_t codes[PG][D / 4 + 1];                // a byte per channel of K
-  __shared__ float sh[4];
+  __shared__ uint32_t s_min[2][D], s_max[2][D];            // [token half][pair of channels, K's then V's]
+  __shared__ __attribute__((aligned(16))) Channel s_ch[2][D];
+  __shared__ _Float16 s_step[2][D];
+  __shared__ float s_top[4];
   const int m = blockIdx.y, tid = threadIdx.x;
   int piece, first, n;
   const int row = row_of_piece(cu, n_rows, n_tokens, blockIdx.x, &piece, &first, &n);
   if (row >= n_rows || piece < 0) return;
   const int s = seqs[row];
   if (s == -1 || n == 0) return;
-  int32_t* const mark_at = c.appended + ((size_t)layer * c.max_seqs + (s < 0 || s >= c.max_seqs ? 0 : s)) * c.n_kv + m;
-  if (s < 0 || s >= c.max_seqs || c.owner[s] != row || c.added[s] != n || *mark_at == c.serial[s]) {
+  const int slot = s < 0 || s >= c.max_seqs ? 0 : s;
+  int32_t* const mark_at = c.appended + ((size_t)layer * c.max_seqs + slot) * c.n_kv + m;
+  const int owner = c.owner[slot], added = c.added[slot], serial = c.serial[slot], marked = *mark_at, end = c.len[slot];
+  if (s != slot || owner != row || added != n || marked == serial) {
     if (piece == 0 && m == 0 && tid == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
     return;
   }
-  const int end = c.len[s], begin = end - n, fills = end / PG - begin / PG;
+  const int begin = end - n, fills = end / PG - begin / PG;
   if (piece >= (fills > 0 ? fills : 1)) return;
   uint16_t* const open = c.open + c.open_at(layer, s, m);
   const size_t stride = (size_t)c.n_kv * D;
@@ -62,71 +87,118 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
 
   if (fills > 0) {
     const int page0 = (begin / PG + piece) * PG;           // first token of the page
-    for (int i = tid; i < 2 * PG * D / 8; i += 256) {
-      const int which = i >> 9, t = (i >> 4) & 31, c8 = i & 15, at = page0 + t;
-      uint4 w;
-      if (at >= begin) {
-        w = load_past((which ? v0 : k0) + (size_t)(at - begin) * stride + c8 * 8);
-      } else if (!which) {
-        w = *reinterpret_cast<const uint4*>(open + t * D + c8 * 8);
-      } else {
-        uint16_t e[8];
+    const int page = c.table[(size_t)s * c.max_pages + page0 / PG];
+    if (page0 >= begin) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = open[open_v_of(t, c8 * 8 + j)];
-        w = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+      for (int j = 0; j < 4; ++j) {
+        const int i = j * 256 + tid, which = i >> 9, t = (i >> 4) & 31, c8 = i & 15;
+        *reinterpret_cast<uint4*>(&tile[which][t][c8 * 8]) = load_past((which ? v0 : k0) + (size_t)(page0 + t - begin) * stride + c8 * 8);
       }
-      *reinterpret_cast<uint4*>(&tile[which][t][c8 * 8]) = w;
+    } else {
+      for (int i = tid; i < 2 * PG * D / 8; i += 256) {
+        const int which = i >> 9, t = (i >> 4) & 31, c8 = i & 15, at = page0 + t;
+        if (at >= begin) *reinterpret_cast<uint4*>(&tile[which][t][c8 * 8]) = load_past((which ? v0 : k0) + (size_t)(at - begin) * stride + c8 * 8);
+        else if (!which) *reinterpret_cast<uint4*>(&tile[0][t][c8 * 8]) = *reinterpret_cast<const uint4*>(open + t * D + c8 * 8);
+      }
+      // the open page's values lie eight tokens to a channel
+      for (int i = tid; i < PG * D / 8; i += 256) {
+        const int kb = i & 3, ch = i >> 2;
+        const uint4 w = *reinterpret_cast<const uint4*>(open + PG * D + (((ch >> 4) * 4 + kb) * 16 + (ch & 15)) * 8);
+        const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = j < 4 ? kb * 4 + j : 12 + kb * 4 + j;
+          if (page0 + t < begin) tile[1][t][ch] = (uint16_t)(e[j >> 1] >> (16 * (j & 1)));
+        }
+      }
     }
     __syncthreads();
 
-    const int which = tid >> 7, ch = tid & 127;
-    const int page = c.table[(size_t)s * c.max_pages + page0 / PG];
+    {
+      const int pair = tid & 127, half = tid >> 7, which = pair >> 6, ch = (pair & 63) * 2;
+      uint32_t lo = in_order(*reinterpret_cast<const uint32_t*>(&tile[which][half * 16][ch])), hi = lo;
+#pragma unroll
+      for (int t = 1; t < 16; ++t) {
+        const uint32_t x = in_order(*reinterpret_cast<const uint32_t*>(&tile[which][half * 16 + t][ch]));
+        lo = min_pair(lo, x);
+        hi = max_pair(hi, x);
+      }
+      s_min[half][pair] = lo;
+      s_max[half][pair] = hi;
+    }
+    __syncthreads();
+
     const size_t u = c.unit(layer, page, m);
     uint8_t* const unit = c.units + u * CU_BYTES;
-    float lo = from_T<DT>(tile[which][0][ch]), hi = lo;
-    bool finite = true;
-#pragma unroll
-    for (int t = 0; t < PG; ++t) {
-      const float x = from_T<DT>(tile[which][t][ch]);
-      finite &= fabsf(x) < INFINITY;
-      lo = fminf(lo, x);
-      hi = fmaxf(hi, x);
+    const int which = tid >> 7, ch = tid & 127;
+    {
+      const int pair = which * 64 + (ch >> 1), sh = (ch & 1) * 16;
+      const uint32_t least = min_pair(s_min[0][pair], s_min[1][pair]), most = max_pair(s_max[0][pair], s_max[1][pair]);
+      const int first_inf = DT == 0 ? 0x7c00 : 0x7f80;     // infinities and NaNs lie from there on, on both sides
+      const bool finite = (int16_t)(most >> sh) < first_inf && (int16_t)(least >> sh) > ~first_inf;
+      const uint16_t lo16 = finite ? (uint16_t)(in_order(least) >> sh) : (uint16_t)0x7fff;      // 0x7fff is a NaN of both types
+      const float lo = from_T<DT>((uint16_t)(in_order(least) >> sh)), hi = from_T<DT>((uint16_t)(in_order(most) >> sh));
+      const float width = finite ? (float)(((double)hi - (double)lo) / 15.0) : 0.f;
+      const float top = wave_max_f32(width);
+      if ((tid & 63) == 0) s_top[tid >> 6] = top;
+      __syncthreads();
+      const float widest = fmaxf(s_top[which * 2], s_top[which * 2 + 1]);
+      const int e = widest > 0.f ? max(ilogbf(widest), -126) : 0;
+      const _Float16 step16 = (_Float16)(width * exp2i(-e));
+      s_ch[which][ch] = Channel{finite ? lo : 0.f, step16 == (_Float16)0 ? 0.f : 1.0f / ldexpf((float)step16, e)};
+      s_step[which][ch] = step16;
+      const int at = which ? vparam_of(ch) : kparam_of(ch);
+      reinterpret_cast<uint16_t*>(unit + (which ? CU_VSTEP : CU_KSTEP))[at] = __builtin_bit_cast(uint16_t, step16);
+      reinterpret_cast<uint16_t*>(unit + (which ? CU_VLO : CU_KLO))[at] = lo16;
+      if (ch == 0) reinterpret_cast<int16_t*>(c.exps + u)[which] = (int16_t)e;
     }
-    const float width = finite ? (float)(((double)hi - (double)lo) / 15.0) : 0.f;
-    const float widest = max_half(width, sh);
-    const int e = widest > 0.f ? max(ilogbf(widest), -126) : 0;
-    const _Float16 step16 = (_Float16)(width * exp2i(-e));
-    Channel q;
-    q.lo = lo;
-    q.step64 = finite ? (double)(float)step16 * ldexp(1.0, e) : 0.0;
-    q.step = (float)q.step64;
-    q.inv = e < -100 ? NAN : 1.0f / q.step;                // (near the end of fp32's range every code is looked at again)
-    const uint16_t lo16 = finite ? to_T<DT>(lo) : (uint16_t)0x7fff;      // 0x7fff is a NaN of both types
-    if (which == 0) {
-#pragma unroll 8
-      for (int t = 0; t < PG; ++t) reinterpret_cast<uint8_t*>(&codes[t][0])[ch] = (uint8_t)q.code(from_T<DT>(tile[0][t][ch]));
-      reinterpret_cast<uint16_t*>(unit + CU_KSTEP)[kparam_of(ch)] = __builtin_bit_cast(uint16_t, step16);
-      reinterpret_cast<uint16_t*>(unit + CU_KLO)[kparam_of(ch)] = lo16;
-    } else {
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w |= q.code(from_T<DT>(tile[1][j < 4 ? kb * 4 + j : 12 + kb * 4 + j][ch])) << (4 * nibble_of(j));
-        reinterpret_cast<uint32_t*>(unit + CU_V)[vword_of(kb, ch)] = w;
-      }
-      reinterpret_cast<uint16_t*>(unit + CU_VSTEP)[vparam_of(ch)] = __builtin_bit_cast(uint16_t, step16);
-      reinterpret_cast<uint16_t*>(unit + CU_VLO)[vparam_of(ch)] = lo16;
-    }
-    if (ch == 0) reinterpret_cast<int16_t*>(c.exps + u)[which] = (int16_t)e;
     __syncthreads();
-    for (int i = tid; i < PG * D / 8; i += 256) {
-      const int mm = (i >> 2) & 15, t = (i >> 8) * 16 + mm, c8 = (i & 3) * 4 + ((i >> 6) & 3);      // (the inverse of kword_of)
-      const uint32_t a = codes[t][c8 * 2], b = codes[t][c8 * 2 + 1];
-      uint32_t w = 0;
+    // the exponents again; near the ends of fp32's range no quotient is good enough, and all are looked at again
+    int exps[2];
+    bool odd[2];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w |= (((j < 4 ? a : b) >> (8 * (j & 3))) & 15u) << (4 * nibble_of(j));
-      reinterpret_cast<uint32_t*>(unit + CU_K)[i] = w;
+    for (int w = 0; w < 2; ++w) {
+      const float top = fmaxf(s_top[w * 2], s_top[w * 2 + 1]);
+      exps[w] = top > 0.f ? max(ilogbf(top), -126) : 0;
+      odd[w] = exps[w] < -100 || exps[w] > 120;
+    }
+    // K: eight channels of two tokens
+    {
+      const int c8 = tid & 15;
+      Channel q[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = s_ch[0][c8 * 8 + j];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int t = h * 16 + (tid >> 4);
+        float x[8], r[8], off = 0.f;
+        unpack8<DT>(*reinterpret_cast<const uint4*>(&tile[0][t][c8 * 8]), x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = code_of(q[j], x[j], off);
+        if (off >= NEAR || odd[0])
+#pragma unroll
+          for (int j = 0; j < 8; ++j) r[j] = code_again(q[j], exps[0], s_step[0][c8 * 8 + j], x[j], r[j], odd[0]);
+        reinterpret_cast<uint32_t*>(unit + CU_K)[kword_of(t, c8)] = word_of(r);
+      }
+    }
+    // V: eight tokens of a channel, twice
+    {
+      const int c1 = tid & 127;
+      const Channel q = s_ch[1][c1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int kb = (tid >> 7) * 2 + h;
+        float x[8], r[8], off = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          x[j] = from_T<DT>(tile[1][j < 4 ? kb * 4 + j : 12 + kb * 4 + j][c1]);
+          r[j] = code_of(q, x[j], off);
+        }
+        if (off >= NEAR || odd[1])
+#pragma unroll
+          for (int j = 0; j < 8; ++j) r[j] = code_again(q, exps[1], s_step[1][c1], x[j], r[j], odd[1]);
+        reinterpret_cast<uint32_t*>(unit + CU_V)[vword_of(kb, c1)] = word_of(r);
+      }
     }
   }
 
@@ -139,7 +211,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
       open[t * D + ch] = k0[(size_t)(at - begin) * stride + ch];
       open[open_v_of(t, ch)] = v0[(size_t)(at - begin) * stride + ch];
     }
-    if (mark && tid == 0) *mark_at = c.serial[s];
+    if (mark && tid == 0) *mark_at = serial;
   }
 }
 
@@ -187,29 +259,39 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDesc c, int layer,
   }
   const size_t u = c.unit(layer, c.table[(size_t)s * c.max_pages + piece], m);
   const uint16_t* const unit = reinterpret_cast<const uint16_t*>(c.units + u * CU_BYTES);
-  for (int i = tid; i < CU_BYTES / 16; i += 256) reinterpret_cast<uint4*>(words)[i] = load_past(unit + i * 8);
   const int32_t e = c.exps[u];
-  const double kscale = ldexp(1.0, (int16_t)(e & 0xffff)), vscale = ldexp(1.0, (int16_t)(e >> 16));
+  for (int i = tid; i < CU_BYTES / 16; i += 256) reinterpret_cast<uint4*>(words)[i] = load_past(unit + i * 8);
   __syncthreads();
+  // A thread has eight channels of two tokens of K and of V, 16 tokens apart: of V they are in the same words.  The value in fp32 (the
+  // product is exact), rounded once more to T.
   const uint16_t* const par = reinterpret_cast<const uint16_t*>(words);
-  // The value in fp32, rounded once more to T.  (A step may be below fp32's normal range, so its exponent is applied in fp64.)
-  for (int i = tid; i < 2 * PG * D / 8; i += 256) {
-    const int which = i >> 9, t = (i >> 4) & 31, c8 = i & 15;
-    if (t >= here) continue;
-    uint32_t out[4];
-    uint16_t r[8];
+  const int c8 = tid & 15, t0 = tid >> 4;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float step[8], lo[8];
+    uint32_t w[8];
+    const int exp = which ? e >> 16 : (int)(int16_t)(e & 0xffff);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int ch = c8 * 8 + j;
-      const int p = which ? vparam_of(ch) : kparam_of(ch);
-      const uint32_t w = which ? words[CU_V / 4 + vword_of(vgroup_of(t), ch)] : words[kword_of(t, c8)];
-      const uint32_t code = (w >> (4 * nibble_of(which ? vplace_of(t) : j))) & 15u;
-      const float step = (float)((double)(float)__builtin_bit_cast(_Float16, par[(which ? CU_VSTEP : CU_KSTEP) / 2 + p]) * (which ? vscale : kscale));
-      r[j] = to_T<DT>(fmaf(step, (float)code, from_T<DT>(par[(which ? CU_VLO : CU_KLO) / 2 + p])));
+      const int ch = c8 * 8 + j, p = which ? vparam_of(ch) : kparam_of(ch);
+      step[j] = ldexpf((float)__builtin_bit_cast(_Float16, par[(which ? CU_VSTEP : CU_KSTEP) / 2 + p]), exp);
+      lo[j] = from_T<DT>(par[(which ? CU_VLO : CU_KLO) / 2 + p]);
+      if (which) w[j] = words[CU_V / 4 + vword_of(vgroup_of(t0), ch)] >> (4 * nibble_of(t0 & 3));
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) out[j] = r[2 * j] | (uint32_t)r[2 * j + 1] << 16;
-    *reinterpret_cast<uint4*>((which ? v0 : k0) + (size_t)t * stride + c8 * 8) = make_uint4(out[0], out[1], out[2], out[3]);
+    for (int h = 0; h < 2; ++h) {
+      const int t = h * 16 + t0;
+      const uint32_t wk = which ? 0 : words[kword_of(t, c8)];
+      uint32_t out[4];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        // (token 16 + t of V: four places on, two nibbles)
+        const uint32_t code = which ? (w[j] >> (4 * (nibble_of(4) * h))) & 15u : (wk >> (4 * nibble_of(j))) & 15u;
+        const uint32_t r = to_T<DT>(fmaf(step[j], (float)code, lo[j]));
+        out[j >> 1] = (j & 1) ? out[j >> 1] | r << 16 : r;
+      }
+      if (t < here) store_past((which ? v0 : k0) + (size_t)t * stride + c8 * 8, make_uint4(out[0], out[1], out[2], out[3]));
+    }
   }
 }
 

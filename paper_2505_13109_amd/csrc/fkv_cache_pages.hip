@@ -41,13 +41,29 @@ __device__ void first_entries(const int32_t* slots, int n, int max_seqs, int* fi
   __syncthreads();
 }
 
-// Takes the `total` lowest free pages of a pool that has as many, and calls got(k, page) for the k-th of them.
+// the n-th (from 0) bit that is set in w
+__device__ __forceinline__ int nth_bit(uint32_t w, int n) {
+  int at = 0;
+#pragma unroll
+  for (int width = 16; width; width >>= 1) {
+    const int below = __popc(w & ((1u << width) - 1));
+    if (n >= below) {
+      n -= below;
+      at += width;
+      w >>= width;
+    }
+  }
+  return at;
+}
+
+// Takes the `total` lowest free pages of a pool that has as many, and calls got(k, page) for the k-th of them.  A thread counts the
+// free pages of a word of 32, then they are dealt out a page to a thread.  The whole block calls it; bits and upto: a word a thread.
 template <typename F>
-__device__ void take_pages(const CacheDesc& c, int total, int* sh, F got) {
-  const int words = (c.n_pages + 31) / 32;
+__device__ void take_pages(const CacheDesc& c, int total, int* sh, uint32_t* bits, int* upto, F got) {
+  const int words = (c.n_pages + 31) / 32, tid = threadIdx.x;
   int done = 0;
-  for (int w0 = 0; w0 < words && done < total; w0 += (int)blockDim.x) {
-    const int w = w0 + (int)threadIdx.x;
+  for (int w0 = 0; w0 < words && done < total; w0 += PLAN_THREADS) {
+    const int w = w0 + tid;
     uint32_t free_bits = 0, old = 0;
     if (w < words) {
       old = c.used[w];
@@ -55,19 +71,27 @@ __device__ void take_pages(const CacheDesc& c, int total, int* sh, F got) {
       if (w == words - 1 && (c.n_pages & 31)) free_bits &= (1u << (c.n_pages & 31)) - 1;
     }
     int here;
-    int k = done + scan_block(__popc(free_bits), &here, sh);
-    uint32_t taken = 0;
-    while (free_bits && k < total) {
-      const int b = __ffs((int)free_bits) - 1;
-      free_bits &= free_bits - 1;
-      taken |= 1u << b;
-      const int page = w * 32 + b;
+    const int before = scan_block(__popc(free_bits), &here, sh);
+    bits[tid] = free_bits;
+    upto[tid] = before + __popc(free_bits);
+    __syncthreads();
+    const int take = min(here, total - done);
+    for (int k = tid; k < take; k += PLAN_THREADS) {
+      int lo = 0, hi = PLAN_THREADS - 1;                   // the first word with more than k free pages up to its end
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (upto[mid] > k) hi = mid; else lo = mid + 1;
+      }
+      const int page = (w0 + lo) * 32 + nth_bit(bits[lo], k - (upto[lo] - __popc(bits[lo])));
       c.ref[page] = 1;
-      got(k, page);
-      ++k;
+      got(done + k, page);
     }
-    if (taken) c.used[w] = old | taken;
+    if (free_bits && before < take) {
+      const int n = min(__popc(free_bits), take - before);
+      c.used[w] = old | (n == __popc(free_bits) ? free_bits : free_bits & ((1u << nth_bit(free_bits, n)) - 1));
+    }
     done += here;
+    __syncthreads();
   }
 }
 
@@ -81,13 +105,15 @@ __device__ int row_of(const int* off, int n, int k) {
   return lo;
 }
 
-// One block: lengths grow, and every row gets the pages that its new tokens fill.  LDS: first[max_seqs], off[n_rows].
+// One block: lengths grow, and every row gets the pages that its new tokens fill.  LDS: first[max_seqs], off[n_rows], base[n_rows].
 __global__ __launch_bounds__(PLAN_THREADS) void cache_extend_kernel(CacheDesc c, const int32_t* __restrict__ seqs, int n_rows,
                                                                     const int32_t* __restrict__ cu) {
   extern __shared__ int lds[];
-  __shared__ int sh[PLAN_THREADS / 64];
+  __shared__ int sh[PLAN_THREADS / 64], upto[PLAN_THREADS];
+  __shared__ uint32_t bits[PLAN_THREADS];
   int* const first = lds;
-  int* const off = lds + c.max_seqs;
+  int* const off = first + c.max_seqs;
+  int* const base = off + n_rows;                          // where in the tables the row's page 0 would go if it were the pool's 0th
   first_entries(seqs, n_rows, c.max_seqs, first);
 
   constexpr int PER = CACHE_MAX_SEQS / PLAN_THREADS;
@@ -117,16 +143,15 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_extend_kernel(CacheDesc c,
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const int i = (int)threadIdx.x * per + j;
-    if (j < per && i < n_rows) off[i] = at;
+    if (j < per && i < n_rows) {
+      off[i] = at;
+      base[i] = slot[j] * c.max_pages + len[j] / PG - at;
+    }
     at += need[j];
   }
   if (total && room) {
     __syncthreads();
-    take_pages(c, total, sh, [&](int k, int page) {
-      const int i = row_of(off, n_rows, k), s = seqs[i];
-      c.table[(size_t)s * c.max_pages + c.len[s] / PG + (k - off[i])] = page;
-    });
-    __syncthreads();      // (the lengths above are the old ones)
+    take_pages(c, total, sh, bits, upto, [&](int k, int page) { c.table[base[row_of(off, n_rows, k)] + k] = page; });
     if (threadIdx.x == 0) c.head[CACHE_USED] += total;
   }
 #pragma unroll
@@ -150,9 +175,10 @@ template <bool COPY>
 __global__ __launch_bounds__(PLAN_THREADS) void cache_fork_kernel(CacheDesc a, const int32_t* __restrict__ src, CacheDesc c,
                                                                   const int32_t* __restrict__ dst, int n) {
   extern __shared__ int lds[];
-  __shared__ int sh[PLAN_THREADS / 64];
+  __shared__ int sh[PLAN_THREADS / 64], upto[COPY ? PLAN_THREADS : 1];
+  __shared__ uint32_t bits[COPY ? PLAN_THREADS : 1];
   int* const first = lds;
-  int* const off = lds + c.max_seqs;
+  int* const off = first + c.max_seqs;
   first_entries(dst, n, c.max_seqs, first);
 
   constexpr int PER = CACHE_MAX_SEQS / PLAN_THREADS;
@@ -185,13 +211,12 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_fork_kernel(CacheDesc a, c
     }
     __syncthreads();
     if (total && room) {
-      take_pages(c, total, sh, [&](int k, int page) {
+      take_pages(c, total, sh, bits, upto, [&](int k, int page) {
         const int i = row_of(off, n, k), pos = k - off[i];
         c.table[(size_t)dst[i] * c.max_pages + pos] = page;
         c.from[k] = a.table[(size_t)src[i] * a.max_pages + pos];
         c.to[k] = page;
       });
-      __syncthreads();
     }
     if (threadIdx.x == 0) {
       if (room) c.head[CACHE_USED] += total;
@@ -313,8 +338,9 @@ __global__ __launch_bounds__(256) void cache_remap_kernel(CacheDesc c) {
   }
 }
 
-// A block per entry: its sequence's pages lose an owner.
-__global__ __launch_bounds__(256) void cache_free_kernel(CacheDesc c, const int32_t* __restrict__ seqs) {
+// A block per entry: its sequence's pages lose an owner.  Four pages a thread at a time: a page is three trips to memory, one behind
+// the other.
+__global__ __launch_bounds__(PLAN_THREADS) void cache_free_kernel(CacheDesc c, const int32_t* __restrict__ seqs) {
   const int i = blockIdx.x, s = seqs[i];
   __shared__ int freed;
   if (s < 0 || s >= c.max_seqs) {
@@ -322,20 +348,28 @@ __global__ __launch_bounds__(256) void cache_free_kernel(CacheDesc c, const int3
     return;
   }
   bool again = false;
-  for (int j = threadIdx.x; j < i; j += 256) again |= seqs[j] == s;
+  for (int j = threadIdx.x; j < i; j += PLAN_THREADS) again |= seqs[j] == s;
   if (threadIdx.x == 0) freed = 0;
   if (__syncthreads_or(again)) {
     if (threadIdx.x == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
     return;
   }
   const int pages = c.len[s] / PG;
+  const int32_t* const table = c.table + (size_t)s * c.max_pages;
   int mine = 0;
-  for (int p = threadIdx.x; p < pages; p += 256) {
-    const int page = c.table[(size_t)s * c.max_pages + p];
-    if (atomicSub(&c.ref[page], 1) == 1) {
-      atomicAnd(&c.used[page >> 5], ~(1u << (page & 31)));
-      ++mine;
-    }
+  constexpr int AT_ONCE = 4;
+  for (int p0 = threadIdx.x; p0 < pages; p0 += PLAN_THREADS * AT_ONCE) {
+    int page[AT_ONCE], left[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) page[j] = p0 + j * PLAN_THREADS < pages ? table[p0 + j * PLAN_THREADS] : -1;
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) left[j] = page[j] >= 0 ? atomicSub(&c.ref[page[j]], 1) : 0;
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j)
+      if (left[j] == 1) {
+        atomicAnd(&c.used[page[j] >> 5], ~(1u << (page[j] & 31)));
+        ++mine;
+      }
   }
   if (mine) atomicAdd(&freed, mine);
   __syncthreads();
@@ -364,7 +398,7 @@ __global__ __launch_bounds__(256) void cache_tables_kernel(CacheDesc c, const in
 }  // namespace
 
 void launch_cache_extend(const CacheDesc& c, const int32_t* seqs, int n_rows, const int32_t* cu, hipStream_t st) {
-  cache_extend_kernel<<<1, PLAN_THREADS, (size_t)(c.max_seqs + n_rows) * 4, st>>>(c, seqs, n_rows, cu);
+  cache_extend_kernel<<<1, PLAN_THREADS, (size_t)(c.max_seqs + 2 * n_rows) * 4, st>>>(c, seqs, n_rows, cu);
 }
 
 void launch_cache_fork(const CacheDesc& c, const int32_t* src, const int32_t* dst, int n, hipStream_t st) {
@@ -380,7 +414,7 @@ void launch_cache_copy(const CacheDesc& from, const int32_t* src, const CacheDes
   cache_open_kernel<<<dim3(to.n_layers * to.n_kv, n), 256, 0, st>>>(from, to, dst, false);
 }
 
-void launch_cache_free(const CacheDesc& c, const int32_t* seqs, int n, hipStream_t st) { cache_free_kernel<<<n, 256, 0, st>>>(c, seqs); }
+void launch_cache_free(const CacheDesc& c, const int32_t* seqs, int n, hipStream_t st) { cache_free_kernel<<<n, PLAN_THREADS, 0, st>>>(c, seqs); }
 
 void launch_cache_compact(const CacheDesc& c, hipStream_t st) {
   cache_compact_kernel<<<1, PLAN_THREADS, 0, st>>>(c);
