@@ -38,16 +38,17 @@ constexpr int CACHE_MAX_G = 16;
 
 struct CacheDesc {
   uint8_t* units;        // [layer][page][n_kv] units
-  int32_t* exps;         // [layer][page][n_kv]: the keys' exponent in the low half, the values' in the high one
+  int32_t* info;         // [layer][page][n_kv]: the unit's exponents, and which use of the page filled it
   uint16_t* open;        // [layer][slot][n_kv] open pages
   int32_t* head;         // CACHE_USED: pages in use; CACHE_FAULTS: FAULT_* bits; CACHE_MOVES: pages on the list of moves
   int32_t* len;          // [slot] tokens
   int32_t* added;        // [slot] tokens of the last extend, and
   int32_t* owner;        // [slot] its row, and
   int32_t* serial;       // [slot] its number, which
-  int32_t* appended;     // [layer][slot][n_kv] takes over when its tokens are there
+  int32_t* appended;     // [layer][slot][n_kv] takes over when the first of its tokens are there
   int32_t* table;        // [slot][max_pages] page ids
   int32_t* ref;          // [page] sequences that share it
+  int32_t* uses;         // [page] how often it has been taken from the pool
   uint32_t* used;        // [(page + 31) / 32] bits: ref > 0
   int32_t* from;         // [page] list of moves: from page
   int32_t* to;           //        to page
@@ -106,6 +107,10 @@ __device__ inline int row_of_piece(const int32_t* cu, int n_rows, int n_tokens, 
   return row;
 }
 inline int cache_pieces(const int32_t* cu, int n_rows, int n_tokens) { return cu ? n_tokens / PG + n_rows : n_rows; }
+
+// A unit's word of info: the keys' exponent, the values', 8 bits each, and the low half of its page's uses when it was filled.
+__device__ __forceinline__ int exp_of_keys(int32_t info) { return (int8_t)(info & 0xff); }
+__device__ __forceinline__ int exp_of_values(int32_t info) { return (int8_t)(info >> 8 & 0xff); }
 
 template <int DT> __device__ __forceinline__ float from_T(uint16_t b) { return Unpack<DT>::one(b); }
 template <int DT> __device__ __forceinline__ uint16_t to_T(float x) {

@@ -50,6 +50,8 @@ size_t lay_out(const fkv_cache_config& c, char* base, CacheDesc* d) {
   take(x.serial, (size_t)c.max_seqs * 4);
   take(x.appended, opens * 4);
   take(x.ref, (size_t)c.n_pages * 4);
+  take(x.uses, (size_t)c.n_pages * 4);
+  take(x.info, units * 4);
   take(x.used, (size_t)(c.n_pages + 31) / 32 * 4);
   take(x.ticket, (size_t)c.max_seqs * c.n_kv_heads * CACHE_TICKETS * 4);
   take(x.table, (size_t)c.max_seqs * x.max_pages * 4);
@@ -60,7 +62,6 @@ size_t lay_out(const fkv_cache_config& c, char* base, CacheDesc* d) {
   take(x.part_ml, items * x.G * 8);
   take(x.group_ml, items * x.G * 8);
   take(x.part, items * x.G * D * 4);
-  take(x.exps, units * 4);
   take(x.open, opens * OPEN_ELEMS * 2);
   take(x.units, units * CU_BYTES);
   if (d) *d = x;

@@ -30,7 +30,7 @@ __device__ __forceinline__ half8 ones_of() { return codes_of(0x11111111u); }
 // The halves of a page of one KV head, as a lane has them.
 struct Keys {
   uint4 k[2], step[4], lo[4];
-  int exps;
+  int info;
 };
 struct Values {
   uint4 v[2], step, lo;
@@ -45,7 +45,7 @@ __device__ __forceinline__ void load_keys(const CacheDesc& c, size_t u, int lane
     r.step[s] = load_past(unit + CU_KSTEP / 2 + kb * 32 + s * 8);
     r.lo[s] = load_past(unit + CU_KLO / 2 + kb * 32 + s * 8);
   }
-  r.exps = c.exps[u];
+  r.info = c.info[u];
 }
 __device__ __forceinline__ void load_values(const CacheDesc& c, size_t u, int lane, Values& r) {
   const uint16_t* const unit = reinterpret_cast<const uint16_t*>(c.units + u * CU_BYTES);
@@ -107,7 +107,7 @@ __device__ __forceinline__ void page_logits(const Keys& r, const half8* q16, con
     x[1] = mfma_h(a1, lo, x[1]);
     bias = mfma_T<DT>(__builtin_bit_cast(u32x4, r.lo[j]), qT[j], bias);
   }
-  const int e = min(max((int)(int16_t)(r.exps & 0xffff) + q_exp, -140), 126);
+  const int e = min(max(exp_of_keys(r.info) + q_exp, -140), 126);
   const float f = ldexpf(scale, e), b = bias[0] * scale;
 #pragma unroll
   for (int mb = 0; mb < 2; ++mb)
@@ -133,12 +133,12 @@ __device__ __forceinline__ half8 page_weights(const f32x4* x, float m) {
 
 // Its values: the weights times the codes, and step and lo of a channel are applied to the page's sums.
 template <int DT>
-__device__ __forceinline__ void page_sums(const Values& r, int exps, half8 p, Seen& s) {
+__device__ __forceinline__ void page_sums(const Values& r, int info, half8 p, Seen& s) {
   const f32x4 none = {0, 0, 0, 0};
   const f32x4 sum = mfma_h(p, ones_of(), none);
   s.l += sum;
   const half8 vstep = __builtin_bit_cast(half8, r.step);
-  const float vscale = ldexpf(1.f, exps >> 16);
+  const float vscale = ldexpf(1.f, exp_of_values(info));
   const uint32_t lo2[4] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w};
   const uint32_t vw[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
 #pragma unroll
@@ -481,21 +481,21 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
       load_keys(c, u, lane, keys);
       load_values(c, u, lane, values);
       f32x4 x[2];
-      int exps;
+      int info;
       while (todo) {
-        exps = keys.exps;
+        info = keys.info;
         page_logits<DT>(keys, q16, qT, q_exp, scale, x);
         u = next();
         load_keys(c, u, lane, keys);
         raise(seen, max8(x), lane);
-        page_sums<DT>(values, exps, page_weights(x, seen.m), seen);
+        page_sums<DT>(values, info, page_weights(x, seen.m), seen);
         load_values(c, u, lane, values);
       }
       // (the last page apart: a load that may or may not be under way would have to be waited for)
-      exps = keys.exps;
+      info = keys.info;
       page_logits<DT>(keys, q16, qT, q_exp, scale, x);
       raise(seen, max8(x), lane);
-      page_sums<DT>(values, exps, page_weights(x, seen.m), seen);
+      page_sums<DT>(values, info, page_weights(x, seen.m), seen);
     }
   }
 

@@ -59,7 +59,7 @@ __device__ __forceinline__ uint32_t word_of(const float* r) {
 template <int DT>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int layer, const int32_t* __restrict__ seqs, int n_rows,
                                                            const int32_t* __restrict__ cu, const uint16_t* __restrict__ K,
-                                                           const uint16_t* __restrict__ V, int n_tokens, bool mark) {
+                                                           const uint16_t* __restrict__ V, int n_tokens) {
   __shared__ __attribute__((aligned(16))) uint16_t tile[2][PG][TILE];
   __shared__ uint32_t s_min[2][D], s_max[2][D];            // [token half][pair of channels, K's then V's]
   __shared__ __attribute__((aligned(16))) Channel s_ch[2][D];
@@ -74,7 +74,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
   const int slot = s < 0 || s >= c.max_seqs ? 0 : s;
   int32_t* const mark_at = c.appended + ((size_t)layer * c.max_seqs + slot) * c.n_kv + m;
   const int owner = c.owner[slot], added = c.added[slot], serial = c.serial[slot], marked = *mark_at, end = c.len[slot];
-  if (s != slot || owner != row || added != n || marked == serial) {
+  // (the mark is the first piece's own: others go by the unit that they fill)
+  if (s != slot || owner != row || added != n || (piece == 0 && marked == serial)) {
     if (piece == 0 && m == 0 && tid == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
     return;
   }
@@ -88,6 +89,9 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
   if (fills > 0) {
     const int page0 = (begin / PG + piece) * PG;           // first token of the page
     const int page = c.table[(size_t)s * c.max_pages + page0 / PG];
+    const size_t u = c.unit(layer, page, m);
+    const int use = c.uses[page] & 0xffff;
+    if ((c.info[u] >> 16 & 0xffff) == use) return;         // filled already since the page was taken
     if (page0 >= begin) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -128,7 +132,6 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
     }
     __syncthreads();
 
-    const size_t u = c.unit(layer, page, m);
     uint8_t* const unit = c.units + u * CU_BYTES;
     const int which = tid >> 7, ch = tid & 127;
     {
@@ -150,7 +153,6 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
       const int at = which ? vparam_of(ch) : kparam_of(ch);
       reinterpret_cast<uint16_t*>(unit + (which ? CU_VSTEP : CU_KSTEP))[at] = __builtin_bit_cast(uint16_t, step16);
       reinterpret_cast<uint16_t*>(unit + (which ? CU_VLO : CU_KLO))[at] = lo16;
-      if (ch == 0) reinterpret_cast<int16_t*>(c.exps + u)[which] = (int16_t)e;
     }
     __syncthreads();
     // the exponents again; near the ends of fp32's range no quotient is good enough, and all are looked at again
@@ -162,6 +164,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
       exps[w] = top > 0.f ? max(ilogbf(top), -126) : 0;
       odd[w] = exps[w] < -100 || exps[w] > 120;
     }
+    if (tid == 0) c.info[u] = (int32_t)((uint32_t)use << 16 | (uint32_t)(exps[1] & 0xff) << 8 | (uint32_t)(exps[0] & 0xff));
     // K: eight channels of two tokens
     {
       const int c8 = tid & 15;
@@ -211,19 +214,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
       open[t * D + ch] = k0[(size_t)(at - begin) * stride + ch];
       open[open_v_of(t, ch)] = v0[(size_t)(at - begin) * stride + ch];
     }
-    if (mark && tid == 0) *mark_at = serial;
+    if (tid == 0) *mark_at = serial;
   }
-}
-
-// Behind an append in which a row may fill several pages: its blocks all look at the mark, so it is set when they are done.
-__global__ __launch_bounds__(256) void cache_mark_kernel(CacheDesc c, int layer, const int32_t* __restrict__ seqs, int n_rows,
-                                                         const int32_t* __restrict__ cu, int n_tokens) {
-  const int i = blockIdx.x * 256 + (int)threadIdx.x, row = i / c.n_kv;
-  if (row >= n_rows) return;
-  const int s = seqs[row];
-  if (s < 0 || s >= c.max_seqs) return;
-  const int a = cu ? min(max(cu[row], 0), n_tokens) : 0, n = cu ? min(max(cu[row + 1], a), n_tokens) - a : 1;
-  if (n > 0 && c.owner[s] == row && c.added[s] == n) c.appended[((size_t)layer * c.max_seqs + s) * c.n_kv + i % c.n_kv] = c.serial[s];
 }
 
 // A block per (page of a row's first tokens, KV head).
@@ -259,7 +251,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDesc c, int layer,
   }
   const size_t u = c.unit(layer, c.table[(size_t)s * c.max_pages + piece], m);
   const uint16_t* const unit = reinterpret_cast<const uint16_t*>(c.units + u * CU_BYTES);
-  const int32_t e = c.exps[u];
+  const int32_t info = c.info[u];
   for (int i = tid; i < CU_BYTES / 16; i += 256) reinterpret_cast<uint4*>(words)[i] = load_past(unit + i * 8);
   __syncthreads();
   // A thread has eight channels of two tokens of K and of V, 16 tokens apart: of V they are in the same words.  The value in fp32 (the
@@ -270,7 +262,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDesc c, int layer,
   for (int which = 0; which < 2; ++which) {
     float step[8], lo[8];
     uint32_t w[8];
-    const int exp = which ? e >> 16 : (int)(int16_t)(e & 0xffff);
+    const int exp = which ? exp_of_values(info) : exp_of_keys(info);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int ch = c8 * 8 + j, p = which ? vparam_of(ch) : kparam_of(ch);
@@ -299,11 +291,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDesc c, int layer,
 
 void launch_cache_append(const CacheDesc& c, int layer, const int32_t* seqs, int n_rows, const int32_t* cu, const uint16_t* k, const uint16_t* v,
                          int n_tokens, hipStream_t st) {
-  const bool several = n_tokens > PG && cu;      // a row may fill more than one page
   const dim3 grid(cache_pieces(cu, n_rows, n_tokens), c.n_kv);
-  if (c.dtype == 0) cache_append_kernel<0><<<grid, 256, 0, st>>>(c, layer, seqs, n_rows, cu, k, v, n_tokens, !several);
-  else cache_append_kernel<1><<<grid, 256, 0, st>>>(c, layer, seqs, n_rows, cu, k, v, n_tokens, !several);
-  if (several) cache_mark_kernel<<<(n_rows * c.n_kv + 255) / 256, 256, 0, st>>>(c, layer, seqs, n_rows, cu, n_tokens);
+  if (c.dtype == 0) cache_append_kernel<0><<<grid, 256, 0, st>>>(c, layer, seqs, n_rows, cu, k, v, n_tokens);
+  else cache_append_kernel<1><<<grid, 256, 0, st>>>(c, layer, seqs, n_rows, cu, k, v, n_tokens);
 }
 
 void launch_cache_read(const CacheDesc& c, int layer, const int32_t* seqs, int n_rows, const int32_t* cu, uint16_t* k, uint16_t* v, int n_tokens,

@@ -84,6 +84,7 @@ __device__ void take_pages(const CacheDesc& c, int total, int* sh, uint32_t* bit
       }
       const int page = (w0 + lo) * 32 + nth_bit(bits[lo], k - (upto[lo] - __popc(bits[lo])));
       c.ref[page] = 1;
+      c.uses[page] += 1;
       got(done + k, page);
     }
     if (free_bits && before < take) {
@@ -278,10 +279,15 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheDesc a, CacheDesc 
     const int layer = (int)(i / moves), k = (int)(i % moves);
     const int f = c.from[k], t = c.to[k];
     copy_words(a.units + a.unit(layer, f, 0) * CU_BYTES, c.units + c.unit(layer, t, 0) * CU_BYTES, words);
-    if ((int)threadIdx.x < c.n_kv) c.exps[c.unit(layer, t, threadIdx.x)] = a.exps[a.unit(layer, f, threadIdx.x)];
+    // a page that moves with its owners is the same use of it; a copy is a use of its own page
+    if ((int)threadIdx.x < c.n_kv) {
+      const int32_t info = a.info[a.unit(layer, f, threadIdx.x)];
+      c.info[c.unit(layer, t, threadIdx.x)] = owners ? info : (int32_t)((uint32_t)c.uses[t] << 16 | (uint32_t)(info & 0xffff));
+    }
     if (owners && layer == 0 && threadIdx.x == 0) {
       c.ref[t] = c.ref[f];
       c.ref[f] = 0;
+      c.uses[t] = c.uses[f];
     }
   }
 }
