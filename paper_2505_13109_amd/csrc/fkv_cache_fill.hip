@@ -27,12 +27,12 @@ __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(short2v, a), __builtin_bit_cast(short2v, b)));
 }
 
-// A channel's codes.  The code is the nearest to the exact quotient: in fp32 the quotient, at most 30, is off by less than 1e-5
-// (three roundings), so only where one comes within 2e-5 of the middle between two codes, it is looked at again in fp64.
+// A channel's codes.  The code is the nearest to the exact quotient.  In fp32 that has three roundings, so at the last border between
+// two codes, 14.5, it is off by less than 2.7e-6: one that comes within 4e-6 of a border is looked at again.
 struct Channel {
   float lo, inv;                   // inv: 1 / step, 0 for a step of 0
 };
-constexpr float NEAR = 0.5f - 2e-5f;
+constexpr float NEAR = 0.5f - 4e-6f;
 // the quotient, at most 15, and the code as a float; off: the furthest that a quotient has been from its code so far
 __device__ __forceinline__ float code_of(const Channel& q, float x, float& off) {
   const float t = fminf((x - q.lo) * q.inv, 15.f);
@@ -40,11 +40,19 @@ __device__ __forceinline__ float code_of(const Channel& q, float x, float& off) 
   off = fmaxf(off, fabsf(t - r));
   return r;
 }
-__device__ __forceinline__ float code_again(const Channel& q, int e, _Float16 step16, float x, float r, bool all) {
-  const float t = fminf((x - q.lo) * q.inv, 15.f);
-  if (step16 == (_Float16)0 || (!all && fabsf(t - r) < NEAR)) return r;
-  const double step = ldexp((double)(float)step16, e);
-  return (float)fmin(rint(((double)x - (double)q.lo) / step), 15.0);
+// Near a border h: the sign of x - lo - h step decides, the even code where it is zero.  That is not rare, one code of 1300 of bf16
+// inputs: steps often are short numbers.  h step has 16 bits and the two are next to each other, so their difference is exact; what
+// x - lo was rounded by is less than that difference's last place and decides only where it is zero.
+__device__ __forceinline__ float code_near(const Channel& q, float step, float x, float r) {
+  const float d = x - q.lo, t = fminf(d * q.inv, 15.f);
+  if (fabsf(t - r) < NEAR) return r;
+  const float b = d - x, err = (x - (d - b)) - (q.lo + b), h = floorf(t) + 0.5f;
+  const float rem = fmaf(-h, step, d) + err;
+  return rem > 0.f ? h + 0.5f : rem < 0.f ? h - 0.5f : rintf(h);
+}
+// in fp64, where a step may be below fp32's normal range or a difference above it
+__device__ __forceinline__ uint32_t code_odd(float x, float lo, _Float16 step16, int e) {
+  return step16 == (_Float16)0 ? 0u : (uint32_t)fmin(rint(((double)x - (double)lo) / ldexp((double)(float)step16, e)), 15.0);
 }
 // eight codes to a word, e = 0..7 at nibble_of(e): sums of sixteen bits are exact in fp32
 __device__ __forceinline__ uint32_t word_of(const float* r) {
@@ -155,7 +163,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
       reinterpret_cast<uint16_t*>(unit + (which ? CU_VLO : CU_KLO))[at] = lo16;
     }
     __syncthreads();
-    // the exponents again; near the ends of fp32's range no quotient is good enough, and all are looked at again
+    // the exponents again; near the ends of fp32's range fp32 will not do
     int exps[2];
     bool odd[2];
 #pragma unroll
@@ -178,10 +186,19 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
         unpack8<DT>(*reinterpret_cast<const uint4*>(&tile[0][t][c8 * 8]), x);
 #pragma unroll
         for (int j = 0; j < 8; ++j) r[j] = code_of(q[j], x[j], off);
-        if (off >= NEAR || odd[0])
+        if (off >= NEAR)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) r[j] = code_again(q[j], exps[0], s_step[0][c8 * 8 + j], x[j], r[j], odd[0]);
-        reinterpret_cast<uint32_t*>(unit + CU_K)[kword_of(t, c8)] = word_of(r);
+          for (int j = 0; j < 8; ++j) r[j] = code_near(q[j], ldexpf((float)s_step[0][c8 * 8 + j], exps[0]), x[j], r[j]);
+        uint32_t w = word_of(r);
+        if (odd[0]) {
+          w = 0;
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j) {
+            const int ch = c8 * 8 + j;
+            w |= code_odd(from_T<DT>(tile[0][t][ch]), s_ch[0][ch].lo, s_step[0][ch], exps[0]) << (4 * nibble_of(j));
+          }
+        }
+        reinterpret_cast<uint32_t*>(unit + CU_K)[kword_of(t, c8)] = w;
       }
     }
     // V: eight tokens of a channel, twice
@@ -197,10 +214,19 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
           x[j] = from_T<DT>(tile[1][j < 4 ? kb * 4 + j : 12 + kb * 4 + j][c1]);
           r[j] = code_of(q, x[j], off);
         }
-        if (off >= NEAR || odd[1])
+        if (off >= NEAR) {
+          const float step = ldexpf((float)s_step[1][c1], exps[1]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) r[j] = code_again(q, exps[1], s_step[1][c1], x[j], r[j], odd[1]);
-        reinterpret_cast<uint32_t*>(unit + CU_V)[vword_of(kb, c1)] = word_of(r);
+          for (int j = 0; j < 8; ++j) r[j] = code_near(q, step, x[j], r[j]);
+        }
+        uint32_t w = word_of(r);
+        if (odd[1]) {
+          w = 0;
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j)
+            w |= code_odd(from_T<DT>(tile[1][j < 4 ? kb * 4 + j : 12 + kb * 4 + j][c1]), q.lo, s_step[1][c1], exps[1]) << (4 * nibble_of(j));
+        }
+        reinterpret_cast<uint32_t*>(unit + CU_V)[vword_of(kb, c1)] = w;
       }
     }
   }

@@ -364,20 +364,28 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_free_kernel(CacheDesc c, c
   const int32_t* const table = c.table + (size_t)s * c.max_pages;
   int mine = 0;
   constexpr int AT_ONCE = 4;
-  for (int p0 = threadIdx.x; p0 < pages; p0 += PLAN_THREADS * AT_ONCE) {
+  const int lane = threadIdx.x & 63;
+  for (int p0 = threadIdx.x - lane; p0 < pages; p0 += PLAN_THREADS * AT_ONCE) {      // (the same for a whole wave)
     int page[AT_ONCE], left[AT_ONCE];
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) page[j] = p0 + j * PLAN_THREADS < pages ? table[p0 + j * PLAN_THREADS] : -1;
+    for (int j = 0; j < AT_ONCE; ++j) page[j] = p0 + lane + j * PLAN_THREADS < pages ? table[p0 + lane + j * PLAN_THREADS] : -1;
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j) left[j] = page[j] >= 0 ? atomicSub(&c.ref[page[j]], 1) : 0;
+    // pages of one word of bits together, which a sequence's mostly are: 64 changes of a word cost 10 us one by one
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j)
-      if (left[j] == 1) {
-        atomicAnd(&c.used[page[j] >> 5], ~(1u << (page[j] & 31)));
-        ++mine;
+    for (int j = 0; j < AT_ONCE; ++j) {
+      unsigned long long todo = __ballot(left[j] == 1);
+      mine += __popcll(todo);
+      while (todo) {
+        const int word = __builtin_amdgcn_readlane(page[j], __ffsll((long long)todo) - 1) >> 5;
+        const bool same = left[j] == 1 && page[j] >> 5 == word;
+        const uint32_t bits = wave_sum_u32(same ? 1u << (page[j] & 31) : 0u);      // (every page once: a sum is an or)
+        if (lane == 0) atomicAnd(&c.used[word], ~bits);
+        todo &= ~__ballot(same);
       }
+    }
   }
-  if (mine) atomicAdd(&freed, mine);
+  if (mine && lane == 0) atomicAdd(&freed, mine);
   __syncthreads();
   if (threadIdx.x == 0) {
     if (freed) atomicSub(&c.head[CACHE_USED], freed);
