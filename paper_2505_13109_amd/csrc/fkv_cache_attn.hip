@@ -211,16 +211,20 @@ constexpr int JOIN = 8, ONE_LEVEL = 12;
 
 // How a row's attention is cut: positions are the pages to attend in order (sink, list, window, or all), the open page last.
 struct Cut {
-  int len, full, sink, win, listed, positions;
-  __device__ __forceinline__ void of(const CacheDesc& c, const CacheAttn& a, int row, int* slot) {
+  int named, slot, len, full, sink, win, listed, positions;      // slot: the one that the row names, -1 if there is no such
+  __device__ __forceinline__ void of(const CacheDesc& c, const CacheAttn& a, int row) {
     const int s = a.seqs[row];
-    *slot = s >= 0 && s < c.max_seqs ? s : -1;
-    len = *slot >= 0 ? c.len[s] : 0;
+    of_slot(a, s, s >= 0 && s < c.max_seqs ? s : -1, s >= 0 && s < c.max_seqs ? c.len[s] : 0);
+  }
+  __device__ __forceinline__ void of_slot(const CacheAttn& a, int seq, int s, int tokens) {
+    named = seq;
+    slot = s;
+    len = tokens;
     full = len / PG;
     if (a.pages) {
       sink = min(a.n_sink, full);
       win = min(a.n_win, full - sink);
-      listed = *slot >= 0 ? a.n_list : 0;
+      listed = slot >= 0 ? a.n_list : 0;
     } else {
       sink = full; win = listed = 0;
     }
@@ -372,10 +376,10 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
   const int item = blockIdx.x / c.n_kv, head = blockIdx.x % c.n_kv, kb = lane >> 4, n = lane & 15;
 
   // -- this block's row and split: every wave by itself up to 64 rows
-  int row = 0, split = item, n_splits, slot;
-  Cut cut;
+  int row = 0, split = item, n_splits;
+  Cut cut = {};
   if (a.n_rows == 1) {
-    cut.of(c, a, 0, &slot);
+    cut.of(c, a, 0);
     n_splits = splits_of(cut.positions, chunk_for(cut.positions, max(CACHE_ATTN_BLOCKS / c.n_kv, 1)));
     if (item >= n_splits) return;
   } else {
@@ -383,14 +387,14 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
     if (a.n_rows <= 64) {
       int mine = 0;
       if (lane < a.n_rows) {
-        cut.of(c, a, lane, &slot);
+        cut.of(c, a, lane);
         mine = cut.positions;
       }
       at = place_of(item, a.n_rows, c.n_kv, lane, [&](int) { return mine; });
     } else {
       int* const s_pos = reinterpret_cast<int*>(s_acc);
       for (int r = tid; r < a.n_rows; r += THREADS) {
-        cut.of(c, a, r, &slot);
+        cut.of(c, a, r);
         s_pos[r] = cut.positions;
       }
       __syncthreads();
@@ -398,9 +402,13 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
     }
     row = at.row; split = at.split; n_splits = at.n_splits;
     if (row < 0) return;
-    cut.of(c, a, row, &slot);
+    if (a.n_rows <= 64)
+      cut.of_slot(a, __builtin_amdgcn_readlane(cut.named, row), __builtin_amdgcn_readlane(cut.slot, row), __builtin_amdgcn_readlane(cut.len, row));
+    else
+      cut.of(c, a, row);
   }
-  if (slot < 0 && head == 0 && tid == 0 && a.seqs[row] != -1) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
+  const int slot = cut.slot;
+  if (slot < 0 && head == 0 && tid == 0 && cut.named != -1) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
   const int size = ((uint32_t)cut.positions + n_splits - 1) / (uint32_t)n_splits;
   const int lo = split * size;
 

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
     const int page = c.table[(size_t)s * c.max_pages + page0 / PG];
     const size_t u = c.unit(layer, page, m);
     const int use = c.uses[page] & 0xffff;
-    if ((c.info[u] >> 16 & 0xffff) == use) return;         // filled already since the page was taken
+    const bool filled = (c.info[u] >> 16 & 0xffff) == use; // already, since the page was taken
     if (page0 >= begin) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -107,20 +107,30 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
         *reinterpret_cast<uint4*>(&tile[which][t][c8 * 8]) = load_past((which ? v0 : k0) + (size_t)(page0 + t - begin) * stride + c8 * 8);
       }
     } else {
-      for (int i = tid; i < 2 * PG * D / 8; i += 256) {
-        const int which = i >> 9, t = (i >> 4) & 31, c8 = i & 15, at = page0 + t;
-        if (at >= begin) *reinterpret_cast<uint4*>(&tile[which][t][c8 * 8]) = load_past((which ? v0 : k0) + (size_t)(at - begin) * stride + c8 * 8);
-        else if (!which) *reinterpret_cast<uint4*>(&tile[0][t][c8 * 8]) = *reinterpret_cast<const uint4*>(open + t * D + c8 * 8);
-      }
-      // the open page's values lie eight tokens to a channel
-      for (int i = tid; i < PG * D / 8; i += 256) {
-        const int kb = i & 3, ch = i >> 2;
-        const uint4 w = *reinterpret_cast<const uint4*>(open + PG * D + (((ch >> 4) * 4 + kb) * 16 + (ch & 15)) * 8);
-        const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+      // the first tokens from the open page, whose values lie eight tokens to a channel; all that is read is on its way at once
+      uint4 w[4], ov[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int t = j < 4 ? kb * 4 + j : 12 + kb * 4 + j;
-          if (page0 + t < begin) tile[1][t][ch] = (uint16_t)(e[j >> 1] >> (16 * (j & 1)));
+      for (int j = 0; j < 4; ++j) {
+        const int i = j * 256 + tid, which = i >> 9, t = (i >> 4) & 31, c8 = i & 15, at = page0 + t;
+        w[j] = make_uint4(0, 0, 0, 0);
+        if (at >= begin) w[j] = load_past((which ? v0 : k0) + (size_t)(at - begin) * stride + c8 * 8);
+        else if (!which) w[j] = *reinterpret_cast<const uint4*>(open + t * D + c8 * 8);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) ov[j] = *reinterpret_cast<const uint4*>(open + PG * D + (j * 256 + tid) * 8);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = j * 256 + tid, which = i >> 9, t = (i >> 4) & 31, c8 = i & 15;
+        if (!which || page0 + t >= begin) *reinterpret_cast<uint4*>(&tile[which][t][c8 * 8]) = w[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int i = j * 256 + tid, kb = (i >> 4) & 3, ch = (i >> 6) * 16 + (i & 15);
+        const uint32_t e[4] = {ov[j].x, ov[j].y, ov[j].z, ov[j].w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int t = k < 4 ? kb * 4 + k : 12 + kb * 4 + k;
+          if (page0 + t < begin) tile[1][t][ch] = (uint16_t)(e[k >> 1] >> (16 * (k & 1)));
         }
       }
     }
@@ -138,6 +148,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
       s_min[half][pair] = lo;
       s_max[half][pair] = hi;
     }
+    if (filled) return;
     __syncthreads();
 
     uint8_t* const unit = c.units + u * CU_BYTES;
