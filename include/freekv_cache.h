@@ -120,7 +120,7 @@ int fkv_cache_free(fkv_cache* cache, const int32_t* seqs_dev, int32_t n, void* s
 int fkv_cache_compact(fkv_cache* cache, void* stream);
 
 /* For each row its sequence's length and page ids: lens_dev dev [n_rows] i32, pages_dev dev [n_rows, max_ctx / page_size] i32,
- * -1 behind the last full page.  Padding: length 0. */
+ * -1 behind the last full page, or NULL: the lengths alone.  Padding: length 0. */
 int fkv_cache_tables(fkv_cache* cache, const int32_t* seqs_dev, int32_t n_rows, int32_t* lens_dev, int32_t* pages_dev,
                      void* stream);
 

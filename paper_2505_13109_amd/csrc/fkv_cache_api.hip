@@ -286,7 +286,7 @@ int fkv_cache_compact(fkv_cache* c, void* stream) {
 int fkv_cache_tables(fkv_cache* c, const int32_t* seqs, int32_t n_rows, int32_t* lens, int32_t* pages, void* stream) {
   FKV_CACHE(c);
   FKV_ROWS(check_rows(c, seqs, n_rows));
-  if (!lens || !pages || !aligned(lens, 4) || !aligned(pages, 4)) return c->fail(FKV_EINVAL, "lengths or pages: null or not 4-byte aligned");
+  if (!lens || !aligned(lens, 4) || !aligned(pages, 4)) return c->fail(FKV_EINVAL, "lengths or pages: null or not 4-byte aligned");
   launch_cache_tables(c->desc, seqs, n_rows, lens, pages, static_cast<hipStream_t>(stream));
   return after_launch(c, "tables kernel");
 }

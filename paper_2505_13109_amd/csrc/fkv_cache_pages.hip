@@ -405,6 +405,7 @@ __global__ __launch_bounds__(256) void cache_tables_kernel(CacheDesc c, const in
     lens[i] = len;
     if (!there && s != -1) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
   }
+  if (!pages) return;
   for (int p = blockIdx.x * 1024 + (int)threadIdx.x; p < min(c.max_pages, ((int)blockIdx.x + 1) * 1024); p += 256)
     pages[(size_t)i * c.max_pages + p] = p < len / PG ? c.table[(size_t)s * c.max_pages + p] : -1;
 }
@@ -437,7 +438,7 @@ void launch_cache_compact(const CacheDesc& c, hipStream_t st) {
 }
 
 void launch_cache_tables(const CacheDesc& c, const int32_t* seqs, int n_rows, int32_t* lens, int32_t* pages, hipStream_t st) {
-  cache_tables_kernel<<<dim3((c.max_pages + 1023) / 1024, n_rows), 256, 0, st>>>(c, seqs, lens, pages);
+  cache_tables_kernel<<<dim3(pages ? (c.max_pages + 1023) / 1024 : 1, n_rows), 256, 0, st>>>(c, seqs, lens, pages);
 }
 
 }  // namespace fkv

@@ -12,20 +12,28 @@ checkpoints here); the cached context of each layer is synthetic and loaded by t
 taken from the caller (seeded synthetic streams with a set adjacent-step similarity) while the projections
 still run and are dropped: that keeps a workload's reuse and correction statistics, which random weights
 would not produce.
+
+Over a `PagedCache` the stack decodes the sequences `seqs` (int32 slots on the GPU) of any lengths: every layer appends its keys and
+values to the 4-bit cache and attends over all of it.  Lengths, and with them the rotary positions, stay on the device, so
+`step()` may be captured into a graph and every replay decodes the next token.
 """
 from __future__ import annotations
 
 import torch
 
 from .binding import FreeKV
+from .paged_cache import PagedCache
 
 
 class DecoderStack:
-    def __init__(self, fkv: FreeKV, *, ffn_mult: float = 3.5, seed: int = 7, rope_base: float = 500000.0,
+    def __init__(self, fkv: FreeKV | PagedCache, *, seqs: torch.Tensor | None = None, ffn_mult: float = 3.5, seed: int = 7, rope_base: float = 500000.0,
                  copy_stream: torch.cuda.Stream | None = None):
         c = fkv.cfg
-        self.fkv = fkv
-        self.n_layers, self.batch = c.n_layers, c.batch
+        self.fkv, self.seqs = fkv, seqs
+        self.paged = isinstance(fkv, PagedCache)
+        if self.paged != (seqs is not None):
+            raise ValueError("a PagedCache, and nothing else, is decoded with the slots of its sequences")
+        self.n_layers, self.batch = c.n_layers, seqs.shape[0] if self.paged else c.batch
         self.n_q, self.n_kv, self.d = c.n_q_heads, c.n_kv_heads, c.head_dim
         self.hidden = self.n_q * self.d
         self.ffn = int(ffn_mult * self.hidden)
@@ -43,7 +51,8 @@ class DecoderStack:
         self.wgu = [mk(self.hidden, 2 * self.ffn, scale=s_in) for _ in range(self.n_layers)]
         self.wd = [mk(self.ffn, self.hidden, scale=self.ffn ** -0.5) for _ in range(self.n_layers)]
         self.inv_freq = (rope_base ** (-torch.arange(0, self.d, 2, device=dev, dtype=torch.float32) / self.d))
-        self.out = torch.empty((self.n_layers, self.batch, self.n_q, self.d), dtype=torch.float32, device=dev)
+        self.out = torch.empty((self.n_layers, self.batch, self.n_q, self.d), dtype=self.dtype if self.paged else torch.float32, device=dev)
+        self.lens = torch.zeros((self.batch,), dtype=torch.int32, device=dev)
         self.copy_stream = copy_stream
         self.last_qkv = [None] * self.n_layers       # what each layer fed to the loop at the last step (for tests)
         self.weight_bytes_per_layer = (self.hidden * qkv_out + self.hidden * self.hidden + 3 * self.hidden * self.ffn) * 2
@@ -59,8 +68,13 @@ class DecoderStack:
     def step(self, x, external_qkv=None, stream=None):
         """x [batch, hidden] -> [batch, hidden].  external_qkv: per layer (q [batch,n_q,d], k, v [batch,n_kv,d])."""
         pos_cached, cos, sin = None, None, None
+        if self.paged:
+            self.fkv.extend(self.seqs, stream=stream)
+            self.fkv.tables(self.seqs, self.lens, stream=stream)
+            ang = (self.lens - 1).float()[:, None, None] * self.inv_freq
+            cos, sin = ang.cos().to(self.dtype), ang.sin().to(self.dtype)
         for layer in range(self.n_layers):
-            pos = self.fkv.context_len(layer)                   # position of the token being appended
+            pos = None if self.paged else self.fkv.context_len(layer)       # position of the token being appended
             if pos != pos_cached:                               # (the layers of one model share it)
                 ang = float(pos) * self.inv_freq
                 cos, sin, pos_cached = ang.cos().to(self.dtype), ang.sin().to(self.dtype), pos
@@ -71,7 +85,11 @@ class DecoderStack:
             if external_qkv is not None:
                 q, k, v = external_qkv[layer]
             self.last_qkv[layer] = (q, k, v)
-            self.fkv.decode_step(layer, q, k, v, self.out[layer], stream=stream, copy_stream=self.copy_stream)
+            if self.paged:
+                self.fkv.append(layer, self.seqs, k, v, stream=stream)
+                self.fkv.attn(layer, self.seqs, q, self.out[layer], stream=stream)
+            else:
+                self.fkv.decode_step(layer, q, k, v, self.out[layer], stream=stream, copy_stream=self.copy_stream)
             x = x + self.out[layer].to(self.dtype).view(self.batch, self.hidden) @ self.wo[layer]
             gu = self._rms(x) @ self.wgu[layer]
             x = x + (torch.nn.functional.silu(gu[:, : self.ffn]) * gu[:, self.ffn:]) @ self.wd[layer]

@@ -128,10 +128,11 @@ class PagedCache:
     def compact(self, stream=None):
         self._check(self.L.fkv_cache_compact(self._h, self._stream(stream)), "fkv_cache_compact")
 
-    def tables(self, seqs, lens, pages, stream=None):
-        """lens [rows], pages [rows, max_ctx // 32] int32"""
+    def tables(self, seqs, lens, pages=None, stream=None):
+        """lens [rows], pages [rows, max_ctx // 32] int32 (None: the lengths alone)"""
         at, n, _ = self._rows(seqs)
-        lens, pages = self._tensor(lens, "lens", torch.int32, (n,)), self._tensor(pages, "pages", torch.int32, (n, self.max_pages))
+        lens = self._tensor(lens, "lens", torch.int32, (n,))
+        pages = None if pages is None else self._tensor(pages, "pages", torch.int32, (n, self.max_pages))
         self._check(self.L.fkv_cache_tables(self._h, at, n, lens, pages, self._stream(stream)), "fkv_cache_tables")
 
     def health(self):

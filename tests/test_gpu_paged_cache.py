@@ -731,3 +731,65 @@ def test_two_caches_at_once_on_two_streams():
     for p, q, o in zip((a, b), qs, outs):
         p.check_attention(0, [0], q=q, got=o[0].cpu())
         assert all(torch.equal(o[0], x) for x in o[1:])
+
+
+# ---- the decoder stack ---------------------------------------------------------------------------------------------
+
+def test_decoder_stack_over_the_cache():
+    """The layers' own keys, values and queries go through the cache: every layer's attention against the model."""
+    from paper_2505_13109_amd.layer_loop import DecoderStack
+    p = Pair(n_layers=3, n_kv=2, G=4, max_seqs=3, max_ctx=256, n_pages=24)
+    p.grow([0, 2], [61, 5])
+    stack = DecoderStack(p.c, seqs=ints([2, 0]), ffn_mult=1.0)
+    x = torch.randn((2, 8 * D), generator=p.gen).bfloat16().cuda()
+    for step in range(5):
+        y = stack.step(x)
+        assert torch.isfinite(y.float()).all() and p.m.extend([2, 0], [1, 1])
+        for layer in range(3):
+            q, k, v = stack.last_qkv[layer]
+            p.m.append(layer, [2, 0], [1, 1], k.cpu(), v.cpu())
+            p.check_attention(layer, [2, 0], q=q.cpu(), got=stack.out[layer].cpu())
+        assert stack.lens.tolist() == [p.m.len[2], p.m.len[0]]
+        x = y
+    p.check_tables()
+    p.check_contents()
+
+
+def test_decoder_stack_in_a_graph_decodes_on():
+    """A branch that is decoded by replays of one captured step gives bit for bit what its sibling gives that is decoded eagerly."""
+    from paper_2505_13109_amd.layer_loop import DecoderStack
+    p = Pair(n_layers=2, n_kv=2, G=4, max_seqs=4, max_ctx=256, n_pages=40)
+    p.grow([0], [58])
+    p.c.fork(ints([0, 0]), ints([1, 2]))
+    eager, captured = (DecoderStack(p.c, seqs=ints([s]), ffn_mult=1.0) for s in (1, 2))
+    x = torch.randn((1, 8 * D), generator=p.gen).bfloat16().cuda()
+    warm = DecoderStack(p.c, seqs=ints([0]), ffn_mult=1.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        warm.step(x)                                     # (the library's products choose their workspaces before a capture)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    xin, graph = x.clone(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        yout = captured.step(xin)
+    a, b = x, x
+    for step in range(40):
+        a = eager.step(a)
+        xin.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        b = yout.clone()
+        assert torch.equal(a, b), step
+    n = ints([1, 2])
+    lens = ints([0, 0])
+    p.c.tables(n, lens)
+    assert lens.tolist() == [98, 98]
+    p.c.health()
+
+
+def test_decoder_stack_wants_the_slots_of_a_cache():
+    from paper_2505_13109_amd.layer_loop import DecoderStack
+    p = Pair(n_kv=2, G=2)
+    with pytest.raises(ValueError):
+        DecoderStack(p.c)
