@@ -235,7 +235,7 @@ int fkv_cache_attn(fkv_cache* c, int32_t layer, const int32_t* seqs, int32_t n_r
   if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return c->fail(FKV_EINVAL, "queries or output: null or not 16-byte aligned");
   if (pages) {
     if (!aligned(pages, 4)) return c->fail(FKV_EINVAL, "page list: not 4-byte aligned");
-    if (n_list < 0 || n_list > c->cfg.max_ctx / PG) return c->fail(FKV_ERANGE, "n_list must be 0 to max_ctx / page_size");
+    if (n_list < 0 || n_list > (1 << 17)) return c->fail(FKV_ERANGE, "n_list must be 0 to 131072");
     if (sink_tokens < 0 || window_tokens < 0 || sink_tokens % PG || window_tokens % PG) return c->fail(FKV_EINVAL, "sink and window must be multiples of page_size");
   } else if (n_list || sink_tokens || window_tokens) {
     return c->fail(FKV_EINVAL, "n_list, sink and window need a page list");

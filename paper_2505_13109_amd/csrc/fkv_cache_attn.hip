@@ -17,15 +17,29 @@ template <int DT> __device__ __forceinline__ f32x4 mfma_T(u32x4 a, u32x4 b, f32x
   else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bfloat8, a), __builtin_bit_cast(bfloat8, b), c, 0, 0, 0);
 }
 
-// Eight codes of a word as fp16 numbers, in five instructions: a nibble left where it is, below the exponent, is a denormal
-// fp16 number, exactly code 2^-24 (e = 0, 1, 4, 5) or code 2^-20 (e = 2, 3, 6, 7); the matrix instruction takes them as they are.
-// The other operand is smaller by 2^-4 at the latter (weight_of).
-__device__ __forceinline__ half8 codes_of(uint32_t w) {
-  const uint32_t h = w >> 8;
-  const u32x4 r = {w & 0x000f000fu, w & 0x00f000f0u, h & 0x000f000fu, h & 0x00f000f0u};
+// Eight codes of a word as fp16 numbers.  Keys', in seven instructions: nibbles are moved to bits 4 to 7 of the half words.  There they
+// are denormal numbers, exactly code 2^-20, and the matrix instruction takes them as they are.
+__device__ __forceinline__ half8 key_codes(uint32_t w) {
+  constexpr uint32_t nibble = 0x00f000f0u;
+  const u32x4 r = {(w << 4) & nibble, w & nibble, (w >> 4) & nibble, (w >> 8) & nibble};
   return __builtin_bit_cast(half8, r);
 }
-__device__ __forceinline__ half8 ones_of() { return codes_of(0x11111111u); }
+// Values', as VALUE_BASE + code.  The instruction cuts products off some 24 bits below the largest one, and takes a denormal number for
+// as large as the smallest normal one.  Logits, whose products have both signs, are off by 1e-5 so; weights, all positive, would lose
+// 2^-15 of their sum on the way, and an output over 128K tokens, small among its values, came out 0.4 % off.
+// 64 + code takes seven instructions and leaves 1e-4 of such an output, for bf16; 16 + code takes eight, for fp16.
+template <int DT> constexpr float VALUE_BASE = DT ? 64.f : 16.f;
+template <int DT> __device__ __forceinline__ half8 value_codes(uint32_t w) {
+  u32x4 r;
+  if constexpr (DT == 1) {
+    constexpr uint32_t nibble = 0x00f000f0u, base = 0x54005400u;
+    r = u32x4{((w << 4) & nibble) | base, (w & nibble) | base, ((w >> 4) & nibble) | base, ((w >> 8) & nibble) | base};
+  } else {
+    constexpr uint32_t nibble = 0x03c003c0u, base = 0x4c004c00u;
+    r = u32x4{((w << 6) & nibble) | base, ((w << 2) & nibble) | base, ((w >> 2) & nibble) | base, ((w >> 6) & nibble) | base};
+  }
+  return __builtin_bit_cast(half8, r);
+}
 
 // The halves of a page of one KV head, as a lane has them.
 struct Keys {
@@ -57,7 +71,7 @@ __device__ __forceinline__ void load_values(const CacheDesc& c, size_t u, int la
 }
 
 // What a wave has seen of a row.  Lane (kb, n): query head n where tokens or channels are the other index of a product, heads
-// 4 kb + i in the sums.  Weights are p = exp2(x - m + HEAD), and sums carry p 2^-24.
+// 4 kb + i in the sums.  Weights are p = exp2(x - m + HEADROOM).
 constexpr float HEADROOM = 7.f;      // weights are at most 2^15 (m may lag 2^8 behind the maximum), fp16's normal range reaches down to 2^-21 of m's
 constexpr float LAG = 8.f;
 struct Seen {
@@ -88,9 +102,10 @@ __device__ __forceinline__ void raise(Seen& s, float top, int lane) {
 }
 
 // A full page's keys: x = q (lo + step code).  The product of q and step is made here, per page and channel, in two fp16 halves
-// (exact: 8 or 11 bits times 11); the codes are the other operand.  x[mb][i]: head n, token mb 16 + kb 4 + i, in powers of two.
+// (exact: 8 or 11 bits times 11); the codes are the other operand.  x[mb][i] is head n's, token mb 16 + kb 4 + i's part of the codes;
+// f x + b is the logit in powers of two.
 template <int DT>
-__device__ __forceinline__ void page_logits(const Keys& r, const half8* q16, const u32x4* qT, int q_exp, float scale, f32x4* x) {
+__device__ __forceinline__ void page_logits(const Keys& r, const half8* q16, const u32x4* qT, int q_exp, float scale, f32x4* x, float* f, float* b) {
   f32x4 bias = {0, 0, 0, 0};
   x[0] = x[1] = bias;
 #pragma unroll
@@ -100,7 +115,7 @@ __device__ __forceinline__ void page_logits(const Keys& r, const half8* q16, con
     const half8 lo = __builtin_elementwise_fma(q16[j], step, -hi);
     const uint32_t w0 = j == 0 ? r.k[0].x : j == 1 ? r.k[0].y : j == 2 ? r.k[0].z : r.k[0].w;
     const uint32_t w1 = j == 0 ? r.k[1].x : j == 1 ? r.k[1].y : j == 2 ? r.k[1].z : r.k[1].w;
-    const half8 a0 = codes_of(w0), a1 = codes_of(w1);
+    const half8 a0 = key_codes(w0), a1 = key_codes(w1);
     x[0] = mfma_h(a0, hi, x[0]);
     x[1] = mfma_h(a1, hi, x[1]);
     x[0] = mfma_h(a0, lo, x[0]);
@@ -108,11 +123,8 @@ __device__ __forceinline__ void page_logits(const Keys& r, const half8* q16, con
     bias = mfma_T<DT>(__builtin_bit_cast(u32x4, r.lo[j]), qT[j], bias);
   }
   const int e = min(max(exp_of_keys(r.info) + q_exp, -140), 126);
-  const float f = ldexpf(scale, e), b = bias[0] * scale;
-#pragma unroll
-  for (int mb = 0; mb < 2; ++mb)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[mb][i] = fmaf(x[mb][i], f, b);
+  *f = ldexpf(scale, e);
+  *b = bias[0] * scale;
 }
 
 __device__ __forceinline__ float max8(const f32x4* x) {
@@ -122,20 +134,34 @@ __device__ __forceinline__ float max8(const f32x4* x) {
   return top;
 }
 
-// Its weights, with what the codes of the other operand want of them: 2^-4 where those are 2^4 larger.
-__device__ __forceinline__ half8 page_weights(const f32x4* x, float m) {
-  const float off0 = m - HEADROOM, off2 = off0 + 4.f;
-  half8 p;
+// Its weights, in fp16, and normalised by the sum of what they were rounded to: half a step of 2^-11 each, 2e-4 of the output on
+// average.  Where the output is fp16 itself, what the rounding left is taken along.
+template <int DT> struct Weights {
+  half8 hi, lo;                      // lo: fp16 only
+};
+template <int DT>
+__device__ __forceinline__ Weights<DT> page_weights(const f32x4* x, float f, float b, float m) {
+  const float off = b - (m - HEADROOM);
+  Weights<DT> p;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) p[j] = (_Float16)__builtin_amdgcn_exp2f(x[j >> 2][j & 3] - ((j & 2) ? off2 : off0));
+  for (int j = 0; j < 8; ++j) {
+    const float w = __builtin_amdgcn_exp2f(fmaf(x[j >> 2][j & 3], f, off));
+    p.hi[j] = (_Float16)w;
+    if constexpr (DT == 0) p.lo[j] = (_Float16)(w - (float)p.hi[j]);
+  }
   return p;
+}
+template <int DT> __device__ __forceinline__ f32x4 weigh(const Weights<DT>& p, half8 v, f32x4 c) {
+  c = mfma_h(p.hi, v, c);
+  if constexpr (DT == 0) c = mfma_h(p.lo, v, c);
+  return c;
 }
 
 // Its values: the weights times the codes, and step and lo of a channel are applied to the page's sums.
 template <int DT>
-__device__ __forceinline__ void page_sums(const Values& r, int info, half8 p, Seen& s) {
-  const f32x4 none = {0, 0, 0, 0};
-  const f32x4 sum = mfma_h(p, ones_of(), none);
+__device__ __forceinline__ void page_sums(const Values& r, int info, const Weights<DT>& p, Seen& s) {
+  const u32x4 ones = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
+  const f32x4 sum = weigh<DT>(p, __builtin_bit_cast(half8, ones), f32x4{0, 0, 0, 0}), base = sum * -VALUE_BASE<DT>;
   s.l += sum;
   const half8 vstep = __builtin_bit_cast(half8, r.step);
   const float vscale = ldexpf(1.f, exp_of_values(info));
@@ -143,7 +169,7 @@ __device__ __forceinline__ void page_sums(const Values& r, int info, half8 p, Se
   const uint32_t vw[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) {
-    const f32x4 pv = mfma_h(p, codes_of(vw[cb]), none);
+    const f32x4 pv = weigh<DT>(p, value_codes<DT>(vw[cb]), base);
     const float step = (float)vstep[cb] * vscale, lo = (cb & 1) ? Unpack<DT>::hi(lo2[cb >> 1]) : Unpack<DT>::lo(lo2[cb >> 1]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) s.acc[cb][i] = fmaf(step, pv[i], fmaf(lo, sum[i], s.acc[cb][i]));
@@ -169,7 +195,7 @@ __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const 
       top = fmaxf(top, x[mb][i]);
     }
   raise(s, top, lane);
-  // weights in T: two halves of bf16 (its 8 bits are fewer than the output's rounding leaves), fp16 as it is
+  // weights in T, and what the rounding left
   const float off = s.m - HEADROOM;
   uint16_t hi[8], lo[8];
   u32x4 there;
@@ -177,7 +203,7 @@ __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const 
   for (int j = 0; j < 8; ++j) {
     const float p = __builtin_amdgcn_exp2f(x[j >> 2][j & 3] - off);
     hi[j] = to_T<DT>(p);
-    lo[j] = DT ? to_T<DT>(p - from_T<DT>(hi[j])) : (uint16_t)0;
+    lo[j] = to_T<DT>(p - from_T<DT>(hi[j]));
   }
   u32x4 ph, pl;
   const uint32_t one = DT == 0 ? 0x3c00u : 0x3f80u;
@@ -190,16 +216,11 @@ __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const 
   }
   const f32x4 none = {0, 0, 0, 0};
   const u32x4 ones = {one | one << 16, one | one << 16, one | one << 16, one | one << 16};
-  f32x4 sum = mfma_T<DT>(ph, ones, none);
-  if constexpr (DT == 1) sum = mfma_T<DT>(pl, ones, sum);
-  constexpr float unit = 1.f / 16777216.f;
-  s.l += sum * unit;
+  s.l += mfma_T<DT>(pl, ones, mfma_T<DT>(ph, ones, none));
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) {
     const u32x4 v = *reinterpret_cast<const u32x4*>(open + PG * D + ((cb * 4 + kb) * 16 + n) * 8) & there;
-    f32x4 pv = mfma_T<DT>(ph, v, none);
-    if constexpr (DT == 1) pv = mfma_T<DT>(pl, v, pv);
-    s.acc[cb] += pv * unit;
+    s.acc[cb] += mfma_T<DT>(pl, v, mfma_T<DT>(ph, v, none));
   }
 }
 
@@ -412,8 +433,8 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
   const int size = ((uint32_t)cut.positions + n_splits - 1) / (uint32_t)n_splits;
   const int lo = split * size;
 
-  // -- the queries: lane (kb, n) has head n's channels 32 j + 8 kb + e, as they are and, further down, as fp16 numbers next
-  //    to 2^13 that carry the codes' weights
+  // -- the queries: lane (kb, n) has head n's channels 32 j + 8 kb + e, as they are and, further down, as fp16 numbers up
+  //    to 2^14
   u32x4 qT[4] = {};
   if (n < c.G) {
     const uint16_t* const q = a.q + ((size_t)row * c.n_kv * c.G + (size_t)head * c.G + n) * D + kb * 8;
@@ -464,11 +485,11 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int e = 13 - q_exp - ((i & 1) ? 4 : 0);
+        const int e = 13 - q_exp;
         q16[j][2 * i] = (_Float16)ldexpf(Unpack<DT>::lo(qT[j][i]), e);
         q16[j][2 * i + 1] = (_Float16)ldexpf(Unpack<DT>::hi(qT[j][i]), e);
       }
-    q_exp += 24 - 13;
+    q_exp += 20 - 13;                                      // (and codes are in units of 2^-20)
   }
 
   // -- the pages
@@ -489,21 +510,22 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
       load_keys(c, u, lane, keys);
       load_values(c, u, lane, values);
       f32x4 x[2];
+      float f, b;
       int info;
       while (todo) {
         info = keys.info;
-        page_logits<DT>(keys, q16, qT, q_exp, scale, x);
+        page_logits<DT>(keys, q16, qT, q_exp, scale, x, &f, &b);
         u = next();
         load_keys(c, u, lane, keys);
-        raise(seen, max8(x), lane);
-        page_sums<DT>(values, info, page_weights(x, seen.m), seen);
+        raise(seen, fmaf(max8(x), f, b), lane);
+        page_sums<DT>(values, info, page_weights<DT>(x, f, b, seen.m), seen);
         load_values(c, u, lane, values);
       }
       // (the last page apart: a load that may or may not be under way would have to be waited for)
       info = keys.info;
-      page_logits<DT>(keys, q16, qT, q_exp, scale, x);
-      raise(seen, max8(x), lane);
-      page_sums<DT>(values, info, page_weights(x, seen.m), seen);
+      page_logits<DT>(keys, q16, qT, q_exp, scale, x, &f, &b);
+      raise(seen, fmaf(max8(x), f, b), lane);
+      page_sums<DT>(values, info, page_weights<DT>(x, f, b, seen.m), seen);
     }
   }
 

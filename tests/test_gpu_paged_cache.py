@@ -271,6 +271,7 @@ def test_attention_over_listed_pages():
     # entries that are none: behind the sequence, in the sink, in the window, below -1; one page twice
     odd = [[[0, 1, 5, 5, 30, 31, 2000000000, -7, 29, 27, 3, -1]] * 2] * 4
     p.check_attention(0, rows, odd, sink=64, window=96)
+    p.check_attention(0, rows, [[[7, -1, 9] * 30] * 2] * 4, sink=32)      # more entries than a sequence has pages
     p.c.health()
 
 
@@ -596,7 +597,6 @@ def test_arguments_are_refused_before_a_launch():
         lambda: c.attn(0, s, q.cpu(), q.clone()), lambda: c.attn(0, s, q, q.clone(), sink=32),
         lambda: c.attn(0, s, q, q.clone(), pages=torch.zeros((2, 2, 3), dtype=torch.int64, device="cuda")),
         lambda: c.attn(0, s, q, q.clone(), pages=torch.zeros((2, 2, 3), dtype=torch.int32, device="cuda"), sink=20),
-        lambda: c.attn(0, s, q, q.clone(), pages=torch.zeros((2, 2, 17), dtype=torch.int32, device="cuda")),
         lambda: c.attn(0, s.long(), q, q.clone()), lambda: c.extend(ints([0] * 5)), lambda: c.extend(s, ints([0, 1])),
         lambda: c.append(0, s, k[:1], k[:1]), lambda: c.append(0, s, k, k[:1]), lambda: c.append(0, s, k.half(), k),
         lambda: c.append(0, s, k.transpose(0, 1), k), lambda: c.append(-1, s, k, k), lambda: c.read(0, s, k[..., :64], k),
