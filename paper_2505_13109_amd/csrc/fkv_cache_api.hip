@@ -24,6 +24,7 @@ const char* check_config(const fkv_cache_config* c) {
   if (c->n_q_heads < c->n_kv_heads || c->n_q_heads % c->n_kv_heads) return "n_q_heads must be a multiple of n_kv_heads";
   if (c->n_q_heads / c->n_kv_heads > CACHE_MAX_G) return "group size above 16 is not supported";
   if (c->max_seqs < 1 || c->max_seqs > CACHE_MAX_SEQS) return "max_seqs must be 1 to 4096";
+  if ((size_t)c->n_layers * c->max_seqs * c->n_kv_heads > (1u << 25)) return "more than 33554432 open pages (layers x slots x KV heads) are not supported";
   if (c->max_ctx < PG || c->max_ctx % PG || c->max_ctx > (1 << 22)) return "max_ctx must be a multiple of page_size, at most 4194304";
   if (c->n_pages < 1 || c->n_pages > (1 << 26)) return "n_pages must be 1 to 67108864";
   if (c->dtype != FKV_DTYPE_FP16 && c->dtype != FKV_DTYPE_BF16) return "dtype must be fp16 or bf16";
@@ -162,6 +163,7 @@ int fkv_cache_create(const fkv_cache_config* cfg, void* dev_arena, size_t dev_by
   lay_out(*cfg, static_cast<char*>(dev_arena), &c->desc);
   hipError_t e = hipGetDevice(&c->device);
   // lengths, counts, tables; what pages and open pages hold is looked at only where these say that something is there
+  if (e == hipSuccess) e = hipDeviceSynchronize();         // (streams of the program may still be using the memory it gives)
   if (e == hipSuccess) e = hipMemset(dev_arena, 0, (size_t)(reinterpret_cast<char*>(c->desc.part) - static_cast<char*>(dev_arena)));
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {

@@ -246,23 +246,11 @@ __device__ __forceinline__ void copy_words(const void* from, void* to, int n) {
   for (int i = threadIdx.x; i < n; i += (int)blockDim.x) t[i] = f[i];
 }
 
-// Open pages of the entries that hold; for a fork also its page table, every page of which gets one more owner.
-// grid (layers x heads, and blocks of 1024 table entries for a fork; entries)
-__global__ __launch_bounds__(256) void cache_open_kernel(CacheDesc a, CacheDesc c, const int32_t* __restrict__ dst, bool share) {
-  const int i = blockIdx.y, s = c.ok[i];
+// An open page of entry i, if it holds: layer and head x.
+__device__ __forceinline__ void copy_open(const CacheDesc& a, const CacheDesc& c, const int32_t* dst, int i, int x) {
+  const int s = c.ok[i];
   if (s < 0) return;
-  const int d = dst[i], len = c.len[d], heads = c.n_layers * c.n_kv;      // (src may be some other entry's dst: what counts is what it was)
-  const int x = blockIdx.x;
-  if (x >= heads) {
-    const int pages = len / PG;
-    for (int p = (x - heads) * 1024 + (int)threadIdx.x; p < min(pages, (x - heads + 1) * 1024); p += 256) {
-      const int page = a.table[(size_t)s * a.max_pages + p];
-      c.table[(size_t)d * c.max_pages + p] = page;
-      if (share) atomicAdd(&c.ref[page], 1);
-    }
-    return;
-  }
-  const int rest = len % PG, layer = x / c.n_kv, m = x % c.n_kv;
+  const int d = dst[i], rest = c.len[d] % PG, layer = x / c.n_kv, m = x % c.n_kv;      // (src may be some other entry's dst: its length may be new)
   if (!rest) return;
   const uint16_t* const f = a.open + a.open_at(layer, s, m);
   uint16_t* const t = c.open + c.open_at(layer, d, m);
@@ -270,21 +258,57 @@ __global__ __launch_bounds__(256) void cache_open_kernel(CacheDesc a, CacheDesc 
   copy_words(f + PG * D, t + PG * D, PG * D / 8);
 }
 
-// Carries the list of moves out, pages of `from` to pages of `to` in all layers; where the pages keep their owners (compact),
-// their counts move too.  Bound by memory.  grid: any number of blocks
-__global__ __launch_bounds__(256) void cache_move_kernel(CacheDesc a, CacheDesc c, bool owners) {
+// Behind a fork's decisions: open pages, and the page table, every page of which gets one more owner.
+// grid (layers x heads, and blocks of 1024 table entries; entries)
+__global__ __launch_bounds__(256) void cache_share_kernel(CacheDesc c, const int32_t* __restrict__ dst) {
+  const int i = blockIdx.y, heads = c.n_layers * c.n_kv;
+  if ((int)blockIdx.x < heads) {
+    copy_open(c, c, dst, i, blockIdx.x);
+    return;
+  }
+  const int s = c.ok[i];
+  if (s < 0) return;
+  const int d = dst[i], pages = c.len[d] / PG, p0 = ((int)blockIdx.x - heads) * 1024;
+  for (int p = p0 + (int)threadIdx.x; p < min(pages, p0 + 1024); p += 256) {
+    const int page = c.table[(size_t)s * c.max_pages + p];
+    c.table[(size_t)d * c.max_pages + p] = page;
+    atomicAdd(&c.ref[page], 1);
+  }
+}
+
+// Carries the list of moves out, pages of `a` to pages of `c` in all layers.  Bound by memory: 4.9 TB/s of reads and writes for 0.34 GB
+// moved, what a copy of one large piece reaches.  The first MOVE_BLOCKS blocks share the moves; those behind
+//   COPY     copy the entries' open pages, one each
+//   compact  give moved pages their new numbers in the page tables, 1024 entries of a slot each
+constexpr int MOVE_BLOCKS = 2048;
+template <bool COPY>
+__global__ __launch_bounds__(256) void cache_move_kernel(CacheDesc a, CacheDesc c, const int32_t* __restrict__ dst) {
   const int moves = c.head[CACHE_MOVES];
+  if (blockIdx.x >= MOVE_BLOCKS) {
+    const int x = (int)blockIdx.x - MOVE_BLOCKS;
+    if (COPY) {
+      copy_open(a, c, dst, x / (c.n_layers * c.n_kv), x % (c.n_layers * c.n_kv));
+    } else if (moves) {
+      const int parts = (c.max_pages + 1023) / 1024, slot = x / parts, p0 = x % parts * 1024, live = c.head[CACHE_USED];
+      const int pages = c.len[slot] / PG;
+      for (int p = p0 + (int)threadIdx.x; p < min(pages, p0 + 1024); p += 256) {
+        int32_t* const e = c.table + (size_t)slot * c.max_pages + p;
+        if (*e >= live) *e = c.remap[*e];
+      }
+    }
+    return;
+  }
   const int words = c.n_kv * CU_BYTES / 16;
-  for (long i = blockIdx.x; i < (long)moves * c.n_layers; i += gridDim.x) {
+  for (long i = blockIdx.x; i < (long)moves * c.n_layers; i += MOVE_BLOCKS) {
     const int layer = (int)(i / moves), k = (int)(i % moves);
     const int f = c.from[k], t = c.to[k];
     copy_words(a.units + a.unit(layer, f, 0) * CU_BYTES, c.units + c.unit(layer, t, 0) * CU_BYTES, words);
     // a page that moves with its owners is the same use of it; a copy is a use of its own page
     if ((int)threadIdx.x < c.n_kv) {
       const int32_t info = a.info[a.unit(layer, f, threadIdx.x)];
-      c.info[c.unit(layer, t, threadIdx.x)] = owners ? info : (int32_t)((uint32_t)c.uses[t] << 16 | (uint32_t)(info & 0xffff));
+      c.info[c.unit(layer, t, threadIdx.x)] = COPY ? (int32_t)((uint32_t)c.uses[t] << 16 | (uint32_t)(info & 0xffff)) : info;
     }
-    if (owners && layer == 0 && threadIdx.x == 0) {
+    if (!COPY && layer == 0 && threadIdx.x == 0) {
       c.ref[t] = c.ref[f];
       c.ref[f] = 0;
       c.uses[t] = c.uses[f];
@@ -331,17 +355,6 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_compact_kernel(CacheDesc c
   for (int w = threadIdx.x; w < words; w += PLAN_THREADS)
     c.used[w] = w * 32 >= live ? 0u : live - w * 32 >= 32 ? ~0u : (1u << (live - w * 32)) - 1;
   if (threadIdx.x == 0) c.head[CACHE_MOVES] = moved;
-}
-
-// Page tables after a compaction: pages behind the ones in use have new numbers.  grid (blocks of 1024 entries, slots)
-__global__ __launch_bounds__(256) void cache_remap_kernel(CacheDesc c) {
-  const int slot = blockIdx.y, live = c.head[CACHE_USED];
-  if (!c.head[CACHE_MOVES]) return;
-  const int pages = c.len[slot] / PG;
-  for (int p = blockIdx.x * 1024 + (int)threadIdx.x; p < min(pages, ((int)blockIdx.x + 1) * 1024); p += 256) {
-    int32_t* const e = c.table + (size_t)slot * c.max_pages + p;
-    if (*e >= live) *e = c.remap[*e];
-  }
 }
 
 // A block per entry: its sequence's pages lose an owner.  Four pages a thread at a time: a page is three trips to memory, one behind
@@ -418,23 +431,19 @@ void launch_cache_extend(const CacheDesc& c, const int32_t* seqs, int n_rows, co
 
 void launch_cache_fork(const CacheDesc& c, const int32_t* src, const int32_t* dst, int n, hipStream_t st) {
   cache_fork_kernel<false><<<1, PLAN_THREADS, (size_t)(c.max_seqs + n) * 4, st>>>(c, src, c, dst, n);
-  cache_open_kernel<<<dim3(c.n_layers * c.n_kv + (c.max_pages + 1023) / 1024, n), 256, 0, st>>>(c, c, dst, true);
+  cache_share_kernel<<<dim3(c.n_layers * c.n_kv + (c.max_pages + 1023) / 1024, n), 256, 0, st>>>(c, dst);
 }
-
-constexpr int MOVE_BLOCKS = 2048;
 
 void launch_cache_copy(const CacheDesc& from, const int32_t* src, const CacheDesc& to, const int32_t* dst, int n, hipStream_t st) {
   cache_fork_kernel<true><<<1, PLAN_THREADS, (size_t)(to.max_seqs + n) * 4, st>>>(from, src, to, dst, n);
-  cache_move_kernel<<<MOVE_BLOCKS, 256, 0, st>>>(from, to, false);
-  cache_open_kernel<<<dim3(to.n_layers * to.n_kv, n), 256, 0, st>>>(from, to, dst, false);
+  cache_move_kernel<true><<<MOVE_BLOCKS + n * to.n_layers * to.n_kv, 256, 0, st>>>(from, to, dst);
 }
 
 void launch_cache_free(const CacheDesc& c, const int32_t* seqs, int n, hipStream_t st) { cache_free_kernel<<<n, PLAN_THREADS, 0, st>>>(c, seqs); }
 
 void launch_cache_compact(const CacheDesc& c, hipStream_t st) {
   cache_compact_kernel<<<1, PLAN_THREADS, 0, st>>>(c);
-  cache_move_kernel<<<MOVE_BLOCKS, 256, 0, st>>>(c, c, true);
-  cache_remap_kernel<<<dim3((c.max_pages + 1023) / 1024, c.max_seqs), 256, 0, st>>>(c);
+  cache_move_kernel<false><<<MOVE_BLOCKS + (c.max_pages + 1023) / 1024 * c.max_seqs, 256, 0, st>>>(c, c, nullptr);
 }
 
 void launch_cache_tables(const CacheDesc& c, const int32_t* seqs, int n_rows, int32_t* lens, int32_t* pages, hipStream_t st) {

@@ -18,7 +18,8 @@ from .binding import CacheConfig, FreeKVError, _ptr, lib
 
 
 class PagedCache:
-    """One cache.  Methods carry the names of the C entry points they call; `stream` None is the current stream of the cache's device."""
+    """One cache.  Methods carry the names of the C entry points they call; `stream` None is the current stream of the cache's device.
+    Tensors are the caller's, to be kept until the stream is done with them."""
 
     def __init__(self, *, n_layers, n_q_heads, n_kv_heads, max_seqs, max_ctx, n_pages, dtype="bf16", head_dim=128, page_size=32, device="cuda:0"):
         self._h = C.c_void_p()

@@ -153,6 +153,24 @@ def test_contents_of_channels_of_very_different_sizes():
     p.check_contents()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_quotients_exactly_between_two_codes(dtype):
+    """A smallest value of 0, a largest of 15 and halves between them: ties go to the even code, and those that a smallest value far below
+    the others' last place moves off the tie do not."""
+    def halves(x, gen):
+        y = torch.randint(0, 31, x.shape, generator=gen).float() / 2
+        y[:, 0], y[:, 1] = 0.0, 15.0
+        y[:, 0, :, 1::4] = -2.0 ** -23                   # (7.5 + 2^-23 is not an fp32 number any more)
+        y[:, 0, :, 2::4] = 2.0 ** -23
+        return y
+
+    p = Pair(n_kv=2, max_seqs=1, dtype=dtype)
+    p.grow([0], [32], halves)
+    p.check_contents()
+    k, _ = p.read(0, [0])
+    assert torch.equal(k[:, :, 0].double(), torch.round(p.m.tokens[0][0][:, 0, :, 0].double()))
+
+
 def test_contents_at_the_ends_of_the_types():
     for dtype, top in (("bf16", 3.0e38), ("fp16", 65504.0)):
         p = Pair(n_kv=1, max_seqs=1, dtype=dtype, seed=3)
@@ -294,6 +312,39 @@ def test_attention_cut_into_many_splits():
     p.check_attention(0, [0])
     p.grow(list(range(1, 40)), [1 + 7 * i for i in range(39)])
     p.check_attention(0, list(range(40)))
+
+
+@pytest.mark.parametrize("kv,rows", [(8, 150), (2, 65), (8, 33)])
+def test_attention_of_many_rows(kv, rows):
+    """More rows than a wave has lanes, and more than there is room to cut each of them."""
+    p = Pair(n_kv=kv, G=2, max_seqs=160, max_ctx=2048, n_pages=2500)
+    lens = [(i * 37) % 400 for i in range(150)] + [2000]
+    seqs = [i for i, n in enumerate(lens) if n]
+    p.grow(seqs, [lens[s] for s in seqs])
+    p.check_attention(0, ([150] + list(range(150)) + [-1])[:rows])
+
+
+def test_as_many_slots_as_there_may_be():
+    p = Pair(n_kv=1, G=1, max_seqs=4096, max_ctx=64, n_pages=5000)
+    first = list(range(2048))
+    k, v = tokens(p.gen, 33, 1, "bf16")
+    k, v = k.repeat(2048, 1, 1), v.repeat(2048, 1, 1)
+    p.c.extend(ints(first), offsets([33] * 2048))
+    assert p.m.extend(first, [33] * 2048)
+    p.c.append(0, ints(first), k.cuda(), v.cuda(), offsets([33] * 2048))
+    p.m.append(0, first, [33] * 2048, k, v)
+    other = list(range(2048, 4096))
+    p.c.fork(ints(first), ints(other))
+    p.m.fork(first, other)
+    p.check_tables()
+    q = p.queries(1).expand(4096, 1, D).contiguous()
+    out = torch.zeros_like(q, device="cuda")
+    p.c.attn(0, ints(list(range(4096))), q.cuda(), out)
+    p.check_attention(0, [17], q=q[:1], got=out[17:18].cpu())
+    assert (out == out[0]).all()
+    p.c.free(ints(first + other))
+    p.m.free(first + other)
+    p.check_tables()
 
 
 def test_attention_is_the_same_every_time():
