@@ -224,10 +224,11 @@ __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const 
   }
 }
 
-// 256 blocks of eight waves take as long (32K tokens 14.6 us against 14.5, 128K x 4 118 against 120) but leave ragged batches less to
-// balance with (33 against 27); three waves to a SIMD, 168 registers, 17.7 and 135.
+// 256 blocks of eight waves take as long (32K tokens, 32/8 heads, 15.4 us either way, 128K x 4 126 against 124) but leave ragged
+// batches less to balance with (36 against 28); three waves to a SIMD, 168 registers and 768 blocks, 19.2, 142 and 34.
 constexpr int WAVES = 4, THREADS = WAVES * 64;
-// Splits that are joined at once, and how many there may be for one level of that.  By 16: 17.3 us for 32K tokens, by 32: 18.1.
+// Splits that are joined at once, and how many there may be for one level of that.  By 16: 32K tokens 16.4 us, lists of 4096 tokens for
+// eight requests 18.6 against 16.0.
 constexpr int JOIN = 8, ONE_LEVEL = 12;
 
 // How a row's attention is cut: positions are the pages to attend in order (sink, list, window, or all), the open page last.
@@ -272,7 +273,7 @@ __device__ __forceinline__ int scan_wave(int v) {
 //
 // There is room for CACHE_ATTN_BLOCKS blocks at once, so for `room` splits of all rows together.  Rows are cut into equal chunks: of a
 // few sizes, from the one that lengths without remainders would allow to the one that any lengths do, the smallest that leaves no
-// split for a second round (32 requests of 500 to 16K tokens, 28/4 heads: 30 us; with about as many splits as there is room
+// split for a second round (32 requests of 500 to 16K tokens, 28/4 heads: 28 us; with about as many splits as there is room
 // 34).  Where there are more rows than half the room, about as many splits as there is room.
 struct Place {
   int row, split, n_splits;
