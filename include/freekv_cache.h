@@ -74,7 +74,8 @@ int fkv_cache_used_pages(fkv_cache* cache);
 
 /* Room for new tokens: row i's sequence becomes cu[i + 1] - cu[i] tokens longer, once for all layers, and gets a page of the
  * pool for every page that these tokens fill: the lowest free ones, in the order of the rows and of their pages.  A row
- * that would pass max_ctx stays as it is; if the pool has too few pages for the others, all stay as they are. */
+ * that would pass max_ctx stays as it is; if the pool has too few pages for the others, all stay as they are.  Until a layer's
+ * fkv_cache_append, the new tokens hold anything in that layer. */
 int fkv_cache_extend(fkv_cache* cache, const int32_t* seqs_dev, int32_t n_rows, const int32_t* cu_dev, void* stream);
 
 /* The new tokens' keys and values in one layer: k, v dev [n_tokens, n_kv, d], 16-byte aligned, row i's being the tokens that its

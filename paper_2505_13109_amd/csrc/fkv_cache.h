@@ -78,7 +78,7 @@ struct CacheAttn {
   const uint16_t* q;
   const int32_t* pages;      // null: every page
   uint16_t* out;
-  int layer, n_rows, n_list, n_sink, n_win, n_items;
+  int layer, n_rows, n_list, n_sink, n_win;
 };
 void launch_cache_attn(const CacheDesc& c, const CacheAttn& a, hipStream_t st);
 void launch_cache_fork(const CacheDesc& c, const int32_t* src, const int32_t* dst, int n, hipStream_t st);

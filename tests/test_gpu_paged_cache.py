@@ -513,6 +513,32 @@ def test_many_pages_are_taken_in_order():
     p.check_tables()
 
 
+def test_pages_past_4_gib():
+    """A pool of 4.6 GB, the first 4.3 of it taken by a sequence that is as long as one may be: the next ones' pages lie behind."""
+    import paper_2505_13109_amd as fkv
+    p = Pair(n_kv=8, G=2, max_seqs=4, max_ctx=4194304, n_pages=112000)
+    assert p.c.dev_bytes > 2 ** 32
+    p.c.extend(ints([0]), offsets([3500000]))            # (its tokens are of no interest)
+    assert p.m.extend([0], [3500000])
+    p.grow([1, 2], [100, 2000])
+    assert min(p.m.pages[1]) * 8 * 5120 > 2 ** 32
+    p.check_contents([1, 2])
+    p.check_attention(0, [2, 1])
+    p.c.copy(ints([1]), ints([3]))
+    assert p.m.copy([1], [3])
+    p.check_contents([3])
+    p.c.free(ints([0]))
+    p.m.free([0])
+    p.c.compact()
+    p.m.compact()
+    assert max(p.m.pages[2]) < 70
+    p.check_contents([1, 2, 3])
+    p.check_attention(0, [2, 1, 3])
+    p.c.extend(ints([0]), offsets([4194305]))
+    with pytest.raises(fkv.FreeKVError, match="max_ctx"):
+        p.c.health()
+
+
 # ---- what the device refuses ------------------------------------------------------------------------------
 
 def _refused(p, match):
