@@ -88,23 +88,48 @@ void launch_cache_compact(const CacheDesc& c, hipStream_t st);
 void launch_cache_tables(const CacheDesc& c, const int32_t* seqs, int n_rows, int32_t* lens, int32_t* pages, hipStream_t st);
 
 // Row and piece of a block among rows of tokens: a row that has n of them has up to n / 32 + 1 pieces (pages that they fill, or touch
-// from a page's begin on), row i's begin at block cu[i] / 32 + i.  first and n: its tokens, held to the n_tokens that there are.
-// The whole block calls it.
-__device__ inline int row_of_piece(const int32_t* cu, int n_rows, int n_tokens, int x, int* piece, int* first, int* n) {
+// from a page's begin on), row i's begin at block cu[i] / 32 + i.  The row's slot is looked up with it: up to 64 rows all are at once, a
+// row to a lane, which is two trips to memory less.  named: what the row names; slot: 0 if there is no such (named tells).
+// first and n: its tokens, held to the n_tokens that there are; len: of the slot.  The whole block calls it.
+struct Piece {
+  int row, piece, first, n, named, slot, len;
+};
+__device__ inline Piece piece_of(const CacheDesc& c, const int32_t* seqs, const int32_t* cu, int n_rows, int n_tokens, int x) {
+  Piece p;
+  auto slot_of = [&](int named) { return named >= 0 && named < c.max_seqs ? named : 0; };
+  if (cu && n_rows <= 64) {
+    const int i = min((int)(threadIdx.x & 63), n_rows - 1);
+    const int named = seqs[i], a = min(max(cu[i], 0), n_tokens), b = min(max(cu[i + 1], a), n_tokens), len = c.len[slot_of(named)];
+    const unsigned long long here = __ballot(a / PG + i <= x && (int)(threadIdx.x & 63) < n_rows);
+    const int r = here ? 63 - __clzll((long long)here) : 0;
+    p.row = r;
+    p.named = __builtin_amdgcn_readlane(named, r);
+    p.first = __builtin_amdgcn_readlane(a, r);
+    p.n = __builtin_amdgcn_readlane(b, r) - p.first;
+    p.len = __builtin_amdgcn_readlane(len, r);
+    p.piece = x - (p.first / PG + r);
+    p.slot = slot_of(p.named);
+    return p;
+  }
   if (!cu) {
-    *piece = 0; *first = x; *n = 1;
-    return x;
+    p.row = p.first = x;
+    p.piece = 0;
+    p.n = 1;
+  } else {
+    int row = -1;
+    for (int i0 = 0; i0 < n_rows; i0 += (int)blockDim.x) {
+      const int i = i0 + (int)threadIdx.x;
+      row += __syncthreads_count(i < n_rows && min(max(cu[min(i, n_rows)], 0), n_tokens) / PG + i <= x);
+    }
+    p.row = max(row, 0);
+    p.first = min(max(cu[p.row], 0), n_tokens);
+    p.n = min(max(cu[p.row + 1], p.first), n_tokens) - p.first;
+    p.piece = x - (p.first / PG + p.row);
   }
-  int row = -1;
-  for (int i0 = 0; i0 < n_rows; i0 += (int)blockDim.x) {
-    const int i = i0 + (int)threadIdx.x;
-    row += __syncthreads_count(i < n_rows && min(max(cu[min(i, n_rows)], 0), n_tokens) / PG + i <= x);
-  }
-  row = max(row, 0);
-  const int a = min(max(cu[row], 0), n_tokens), b = min(max(cu[row + 1], a), n_tokens);
-  *piece = x - (a / PG + row);
-  *first = a; *n = b - a;
-  return row;
+  p.named = seqs[p.row];
+  p.slot = slot_of(p.named);
+  p.len = c.len[p.slot];
+  return p;
 }
 inline int cache_pieces(const int32_t* cu, int n_rows, int n_tokens) { return cu ? n_tokens / PG + n_rows : n_rows; }
 

@@ -74,14 +74,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
   __shared__ _Float16 s_step[2][D];
   __shared__ float s_top[4];
   const int m = blockIdx.y, tid = threadIdx.x;
-  int piece, first, n;
-  const int row = row_of_piece(cu, n_rows, n_tokens, blockIdx.x, &piece, &first, &n);
-  if (row >= n_rows || piece < 0) return;
-  const int s = seqs[row];
-  if (s == -1 || n == 0) return;
-  const int slot = s < 0 || s >= c.max_seqs ? 0 : s;
+  const Piece at_row = piece_of(c, seqs, cu, n_rows, n_tokens, blockIdx.x);
+  const int row = at_row.row, piece = at_row.piece, first = at_row.first, n = at_row.n, s = at_row.named, slot = at_row.slot, end = at_row.len;
+  if (piece < 0 || s == -1 || n == 0) return;
   int32_t* const mark_at = c.appended + ((size_t)layer * c.max_seqs + slot) * c.n_kv + m;
-  const int owner = c.owner[slot], added = c.added[slot], serial = c.serial[slot], marked = *mark_at, end = c.len[slot];
+  const int owner = c.owner[slot], added = c.added[slot], serial = c.serial[slot], marked = *mark_at;
   // (the mark is the first piece's own: others go by the unit that they fill)
   if (s != slot || owner != row || added != n || (piece == 0 && marked == serial)) {
     if (piece == 0 && m == 0 && tid == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
@@ -262,15 +259,14 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDesc c, int layer,
                                                          uint16_t* __restrict__ V, int n_tokens) {
   __shared__ __attribute__((aligned(16))) uint32_t words[CU_BYTES / 4];
   const int m = blockIdx.y, tid = threadIdx.x;
-  int piece, first, n;
-  const int row = row_of_piece(cu, n_rows, n_tokens, blockIdx.x, &piece, &first, &n);
-  if (row >= n_rows || piece < 0) return;
-  const int s = seqs[row];
-  if (s < 0 || s >= c.max_seqs) {
-    if (s != -1 && piece == 0 && m == 0 && tid == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
+  const Piece at_row = piece_of(c, seqs, cu, n_rows, n_tokens, blockIdx.x);
+  const int piece = at_row.piece, first = at_row.first, s = at_row.slot, len = at_row.len;
+  if (piece < 0) return;
+  if (at_row.named != s) {
+    if (at_row.named != -1 && piece == 0 && m == 0 && tid == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
     return;
   }
-  const int len = c.len[s], end = min(n, len), page0 = piece * PG;
+  const int end = min(at_row.n, len), page0 = piece * PG;
   if (page0 >= end) return;
   const int here = min(PG, end - page0);
   const size_t stride = (size_t)c.n_kv * D;
