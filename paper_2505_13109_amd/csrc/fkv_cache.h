@@ -90,10 +90,12 @@ void launch_cache_tables(const CacheDesc& c, const int32_t* seqs, int n_rows, in
 // Row and piece of a block among rows of tokens: a row that has n of them has up to n / 32 + 1 pieces (pages that they fill, or touch
 // from a page's begin on), row i's begin at block cu[i] / 32 + i.  The row's slot is looked up with it: up to 64 rows all are at once, a
 // row to a lane, which is two trips to memory less.  named: what the row names; slot: 0 if there is no such (named tells).
-// first and n: its tokens, held to the n_tokens that there are; len: of the slot.  The whole block calls it.
+// first and n: its tokens, held to the n_tokens that there are; len: of the slot.  PAGE: also the piece-th entry of the slot's page
+// table, whatever it holds, asked for beside the length.  The whole block calls it.
 struct Piece {
-  int row, piece, first, n, named, slot, len;
+  int row, piece, first, n, named, slot, len, page;
 };
+template <bool PAGE>
 __device__ inline Piece piece_of(const CacheDesc& c, const int32_t* seqs, const int32_t* cu, int n_rows, int n_tokens, int x) {
   Piece p;
   auto slot_of = [&](int named) { return named >= 0 && named < c.max_seqs ? named : 0; };
@@ -106,9 +108,10 @@ __device__ inline Piece piece_of(const CacheDesc& c, const int32_t* seqs, const 
     p.named = __builtin_amdgcn_readlane(named, r);
     p.first = __builtin_amdgcn_readlane(a, r);
     p.n = __builtin_amdgcn_readlane(b, r) - p.first;
-    p.len = __builtin_amdgcn_readlane(len, r);
     p.piece = x - (p.first / PG + r);
     p.slot = slot_of(p.named);
+    if (PAGE) p.page = c.table[(size_t)p.slot * c.max_pages + min(max(p.piece, 0), c.max_pages - 1)];
+    p.len = __builtin_amdgcn_readlane(len, r);
     return p;
   }
   if (!cu) {
@@ -128,6 +131,7 @@ __device__ inline Piece piece_of(const CacheDesc& c, const int32_t* seqs, const 
   }
   p.named = seqs[p.row];
   p.slot = slot_of(p.named);
+  if (PAGE) p.page = c.table[(size_t)p.slot * c.max_pages + min(max(p.piece, 0), c.max_pages - 1)];
   p.len = c.len[p.slot];
   return p;
 }

@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
   __shared__ _Float16 s_step[2][D];
   __shared__ float s_top[4];
   const int m = blockIdx.y, tid = threadIdx.x;
-  const Piece at_row = piece_of(c, seqs, cu, n_rows, n_tokens, blockIdx.x);
+  const Piece at_row = piece_of<false>(c, seqs, cu, n_rows, n_tokens, blockIdx.x);
   const int row = at_row.row, piece = at_row.piece, first = at_row.first, n = at_row.n, s = at_row.named, slot = at_row.slot, end = at_row.len;
   if (piece < 0 || s == -1 || n == 0) return;
   int32_t* const mark_at = c.appended + ((size_t)layer * c.max_seqs + slot) * c.n_kv + m;
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDesc c, int layer,
                                                          uint16_t* __restrict__ V, int n_tokens) {
   __shared__ __attribute__((aligned(16))) uint32_t words[CU_BYTES / 4];
   const int m = blockIdx.y, tid = threadIdx.x;
-  const Piece at_row = piece_of(c, seqs, cu, n_rows, n_tokens, blockIdx.x);
+  const Piece at_row = piece_of<true>(c, seqs, cu, n_rows, n_tokens, blockIdx.x);
   const int piece = at_row.piece, first = at_row.first, s = at_row.slot, len = at_row.len;
   if (piece < 0) return;
   if (at_row.named != s) {
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDesc c, int layer,
     }
     return;
   }
-  const size_t u = c.unit(layer, c.table[(size_t)s * c.max_pages + piece], m);
+  const size_t u = c.unit(layer, at_row.page, m);
   const uint16_t* const unit = reinterpret_cast<const uint16_t*>(c.units + u * CU_BYTES);
   const int32_t info = c.info[u];
   for (int i = tid; i < CU_BYTES / 16; i += 256) reinterpret_cast<uint4*>(words)[i] = load_past(unit + i * 8);

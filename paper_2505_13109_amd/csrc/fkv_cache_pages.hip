@@ -57,16 +57,17 @@ __device__ __forceinline__ int nth_bit(uint32_t w, int n) {
 }
 
 // Takes the `total` lowest free pages of a pool that has as many, and calls got(k, page) for the k-th of them.  A thread counts the
-// free pages of a word of 32, then they are dealt out a page to a thread.  The whole block calls it; bits and upto: a word a thread.
+// free pages of a word of 32, then they are dealt out a page to a thread.  The whole block calls it; bits and upto: a word a thread;
+// word0: this thread's first one, which the caller has asked for early.
 template <typename F>
-__device__ void take_pages(const CacheDesc& c, int total, int* sh, uint32_t* bits, int* upto, F got) {
+__device__ void take_pages(const CacheDesc& c, int total, uint32_t word0, int* sh, uint32_t* bits, int* upto, F got) {
   const int words = (c.n_pages + 31) / 32, tid = threadIdx.x;
   int done = 0;
   for (int w0 = 0; w0 < words && done < total; w0 += PLAN_THREADS) {
     const int w = w0 + tid;
     uint32_t free_bits = 0, old = 0;
     if (w < words) {
-      old = c.used[w];
+      old = w0 ? c.used[w] : word0;
       free_bits = ~old;
       if (w == words - 1 && (c.n_pages & 31)) free_bits &= (1u << (c.n_pages & 31)) - 1;
     }
@@ -84,7 +85,7 @@ __device__ void take_pages(const CacheDesc& c, int total, int* sh, uint32_t* bit
       }
       const int page = (w0 + lo) * 32 + nth_bit(bits[lo], k - (upto[lo] - __popc(bits[lo])));
       c.ref[page] = 1;
-      c.uses[page] += 1;
+      atomicAdd(&c.uses[page], 1);                         // (by itself: nothing waits for it)
       got(done + k, page);
     }
     if (free_bits && before < take) {
@@ -115,6 +116,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_extend_kernel(CacheDesc c,
   int* const first = lds;
   int* const off = first + c.max_seqs;
   int* const base = off + n_rows;                          // where in the tables the row's page 0 would go if it were the pool's 0th
+  const int in_use = c.head[CACHE_USED];
+  const uint32_t word0 = (int)threadIdx.x < (c.n_pages + 31) / 32 ? c.used[threadIdx.x] : 0u;
   first_entries(seqs, n_rows, c.max_seqs, first);
 
   constexpr int PER = CACHE_MAX_SEQS / PLAN_THREADS;
@@ -139,7 +142,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_extend_kernel(CacheDesc c,
   }
   int total;
   int at = scan_block(mine, &total, sh);
-  const bool room = total <= c.n_pages - c.head[CACHE_USED];
+  const bool room = total <= c.n_pages - in_use;
   if (!room) faults |= FAULT_PAGES;
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
@@ -152,8 +155,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_extend_kernel(CacheDesc c,
   }
   if (total && room) {
     __syncthreads();
-    take_pages(c, total, sh, bits, upto, [&](int k, int page) { c.table[base[row_of(off, n_rows, k)] + k] = page; });
-    if (threadIdx.x == 0) c.head[CACHE_USED] += total;
+    take_pages(c, total, word0, sh, bits, upto, [&](int k, int page) { c.table[base[row_of(off, n_rows, k)] + k] = page; });
+    if (threadIdx.x == 0) c.head[CACHE_USED] = in_use + total;
   }
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
@@ -180,6 +183,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_fork_kernel(CacheDesc a, c
   __shared__ uint32_t bits[COPY ? PLAN_THREADS : 1];
   int* const first = lds;
   int* const off = first + c.max_seqs;
+  const int in_use = COPY ? c.head[CACHE_USED] : 0;
+  const uint32_t word0 = COPY && (int)threadIdx.x < (c.n_pages + 31) / 32 ? c.used[threadIdx.x] : 0u;
   first_entries(dst, n, c.max_seqs, first);
 
   constexpr int PER = CACHE_MAX_SEQS / PLAN_THREADS;
@@ -202,7 +207,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_fork_kernel(CacheDesc a, c
   bool room = true;
   if (COPY) {
     at = scan_block(mine, &total, sh);
-    room = total <= c.n_pages - c.head[CACHE_USED];
+    room = total <= c.n_pages - in_use;
     if (!room) faults |= FAULT_PAGES;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -212,7 +217,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_fork_kernel(CacheDesc a, c
     }
     __syncthreads();
     if (total && room) {
-      take_pages(c, total, sh, bits, upto, [&](int k, int page) {
+      take_pages(c, total, word0, sh, bits, upto, [&](int k, int page) {
         const int i = row_of(off, n, k), pos = k - off[i];
         c.table[(size_t)dst[i] * c.max_pages + pos] = page;
         c.from[k] = a.table[(size_t)src[i] * a.max_pages + pos];
@@ -220,7 +225,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_fork_kernel(CacheDesc a, c
       });
     }
     if (threadIdx.x == 0) {
-      if (room) c.head[CACHE_USED] += total;
+      if (room) c.head[CACHE_USED] = in_use + total;
       c.head[CACHE_MOVES] = room ? total : 0;
     }
   } else {
@@ -373,15 +378,19 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_free_kernel(CacheDesc c, c
     if (threadIdx.x == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
     return;
   }
-  const int pages = c.len[s] / PG;
   const int32_t* const table = c.table + (size_t)s * c.max_pages;
+  const int32_t first_page = (int)threadIdx.x < c.max_pages ? table[threadIdx.x] : -1;      // (asked for beside the length)
+  const int pages = c.len[s] / PG;
   int mine = 0;
   constexpr int AT_ONCE = 4;
   const int lane = threadIdx.x & 63;
   for (int p0 = threadIdx.x - lane; p0 < pages; p0 += PLAN_THREADS * AT_ONCE) {      // (the same for a whole wave)
     int page[AT_ONCE], left[AT_ONCE];
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) page[j] = p0 + lane + j * PLAN_THREADS < pages ? table[p0 + lane + j * PLAN_THREADS] : -1;
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int p = p0 + lane + j * PLAN_THREADS;
+      page[j] = p >= pages ? -1 : p < PLAN_THREADS ? first_page : table[p];
+    }
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j) left[j] = page[j] >= 0 ? atomicSub(&c.ref[page[j]], 1) : 0;
     // pages of one word of bits together, which a sequence's mostly are: 64 changes of a word cost 10 us one by one
@@ -413,14 +422,20 @@ __global__ __launch_bounds__(256) void cache_tables_kernel(CacheDesc c, const in
                                                            int32_t* __restrict__ pages) {
   const int i = blockIdx.y, s = seqs[i];
   const bool there = s >= 0 && s < c.max_seqs;
-  const int len = there ? c.len[s] : 0;
+  const int len = there ? c.len[s] : 0, p0 = blockIdx.x * 1024 + (int)threadIdx.x;
+  if (pages) {
+    const int32_t* const table = c.table + (size_t)(there ? s : 0) * c.max_pages;
+    int32_t page[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) page[j] = p0 + j * 256 < c.max_pages ? table[p0 + j * 256] : 0;      // (whether or not one is there)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (p0 + j * 256 < c.max_pages) pages[(size_t)i * c.max_pages + p0 + j * 256] = p0 + j * 256 < len / PG ? page[j] : -1;
+  }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     lens[i] = len;
     if (!there && s != -1) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
   }
-  if (!pages) return;
-  for (int p = blockIdx.x * 1024 + (int)threadIdx.x; p < min(c.max_pages, ((int)blockIdx.x + 1) * 1024); p += 256)
-    pages[(size_t)i * c.max_pages + p] = p < len / PG ? c.table[(size_t)s * c.max_pages + p] : -1;
 }
 
 }  // namespace
