@@ -28,14 +28,21 @@ __device__ __forceinline__ half8 key_codes(uint32_t w) {
 // as large as the smallest normal one.  Logits, whose products have both signs, are off by 1e-5 so; weights, all positive, would lose
 // 2^-15 of their sum on the way, and an output over 128K tokens, small among its values, came out 0.4 % off.
 // 64 + code takes seven instructions and leaves 1e-4 of such an output, for bf16; 16 + code takes eight, for fp16.
+// (The base's bits come from a register that is not known to be a constant: an instruction takes one constant, and masking and
+// setting are one of three operands so, 32 fewer to a page, 373 -> 341.)
 template <int DT> constexpr float VALUE_BASE = DT ? 64.f : 16.f;
-template <int DT> __device__ __forceinline__ half8 value_codes(uint32_t w) {
+template <int DT> __device__ __forceinline__ uint32_t value_bits() {
+  uint32_t b = DT ? 0x54005400u : 0x4c004c00u;
+  asm("" : "+v"(b));
+  return b;
+}
+template <int DT> __device__ __forceinline__ half8 value_codes(uint32_t w, uint32_t base) {
   u32x4 r;
   if constexpr (DT == 1) {
-    constexpr uint32_t nibble = 0x00f000f0u, base = 0x54005400u;
+    constexpr uint32_t nibble = 0x00f000f0u;
     r = u32x4{((w << 4) & nibble) | base, (w & nibble) | base, ((w >> 4) & nibble) | base, ((w >> 8) & nibble) | base};
   } else {
-    constexpr uint32_t nibble = 0x03c003c0u, base = 0x4c004c00u;
+    constexpr uint32_t nibble = 0x03c003c0u;
     r = u32x4{((w << 6) & nibble) | base, ((w << 2) & nibble) | base, ((w >> 2) & nibble) | base, ((w >> 6) & nibble) | base};
   }
   return __builtin_bit_cast(half8, r);
@@ -159,7 +166,7 @@ template <int DT> __device__ __forceinline__ f32x4 weigh(const Weights<DT>& p, h
 
 // Its values: the weights times the codes, and step and lo of a channel are applied to the page's sums.
 template <int DT>
-__device__ __forceinline__ void page_sums(const Values& r, int info, const Weights<DT>& p, Seen& s) {
+__device__ __forceinline__ void page_sums(const Values& r, int info, const Weights<DT>& p, uint32_t bits, Seen& s) {
   const u32x4 ones = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
   const f32x4 sum = weigh<DT>(p, __builtin_bit_cast(half8, ones), f32x4{0, 0, 0, 0}), base = sum * -VALUE_BASE<DT>;
   s.l += sum;
@@ -169,7 +176,7 @@ __device__ __forceinline__ void page_sums(const Values& r, int info, const Weigh
   const uint32_t vw[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) {
-    const f32x4 pv = weigh<DT>(p, value_codes<DT>(vw[cb]), base);
+    const f32x4 pv = weigh<DT>(p, value_codes<DT>(vw[cb], bits), base);
     const float step = (float)vstep[cb] * vscale, lo = (cb & 1) ? Unpack<DT>::hi(lo2[cb >> 1]) : Unpack<DT>::lo(lo2[cb >> 1]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) s.acc[cb][i] = fmaf(step, pv[i], fmaf(lo, sum[i], s.acc[cb][i]));
@@ -494,6 +501,7 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
   }
 
   // -- the pages
+  const uint32_t bits = value_bits<DT>();
   for (int p0 = lo + turn; p0 < hi; p0 += 64 * WAVES) {
     if (p0 > lo + turn) page = page_at(p0);
     unsigned long long todo = __ballot(page >= 0);
@@ -519,14 +527,14 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
         u = next();
         load_keys(c, u, lane, keys);
         raise(seen, fmaf(max8(x), f, b), lane);
-        page_sums<DT>(values, info, page_weights<DT>(x, f, b, seen.m), seen);
+        page_sums<DT>(values, info, page_weights<DT>(x, f, b, seen.m), bits, seen);
         load_values(c, u, lane, values);
       }
       // (the last page apart: a load that may or may not be under way would have to be waited for)
       info = keys.info;
       page_logits<DT>(keys, q16, qT, q_exp, scale, x, &f, &b);
       raise(seen, fmaf(max8(x), f, b), lane);
-      page_sums<DT>(values, info, page_weights<DT>(x, f, b, seen.m), seen);
+      page_sums<DT>(values, info, page_weights<DT>(x, f, b, seen.m), bits, seen);
     }
   }
 
