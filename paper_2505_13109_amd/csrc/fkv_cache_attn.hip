@@ -523,7 +523,10 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
       int info;
       while (todo) {
         info = keys.info;
+        // (logits before another wave's sums, so that its next loads are asked for soon: 1 to 3 %)
+        __builtin_amdgcn_s_setprio(1);
         page_logits<DT>(keys, q16, qT, q_exp, scale, x, &f, &b);
+        __builtin_amdgcn_s_setprio(0);
         u = next();
         load_keys(c, u, lane, keys);
         raise(seen, fmaf(max8(x), f, b), lane);
