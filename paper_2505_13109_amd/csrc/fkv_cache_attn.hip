@@ -81,6 +81,7 @@ __device__ __forceinline__ void load_values(const CacheDesc& c, size_t u, int la
 // 4 kb + i in the sums.  Weights are p = exp2(x - m + HEADROOM).
 constexpr float HEADROOM = 7.f;      // weights are at most 2^15 (m may lag 2^8 behind the maximum), fp16's normal range reaches down to 2^-21 of m's
 constexpr float LAG = 8.f;
+constexpr float LARGEST = 15.99f;
 struct Seen {
   float m;                           // of head n, in powers of two
   f32x4 l, acc[8];                   // of head 4 kb + i; channels cb 16 + n
@@ -142,7 +143,8 @@ __device__ __forceinline__ float max8(const f32x4* x) {
 }
 
 // Its weights, in fp16, and normalised by the sum of what they were rounded to: half a step of 2^-11 each, 2e-4 of the output on
-// average.  Where the output is fp16 itself, what the rounding left is taken along.
+// average.  Where the output is fp16 itself, what the rounding left is taken along.  Logits past 2^22 are so far apart in fp32 that a
+// weight may come out at 2^16, which fp16 does not have: it is held to what there is (a NaN stays one).
 template <int DT> struct Weights {
   half8 hi, lo;                      // lo: fp16 only
 };
@@ -152,7 +154,7 @@ __device__ __forceinline__ Weights<DT> page_weights(const f32x4* x, float f, flo
   Weights<DT> p;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float w = __builtin_amdgcn_exp2f(fmaf(x[j >> 2][j & 3], f, off));
+    const float w = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(fmaf(x[j >> 2][j & 3], f, off), LARGEST));
     p.hi[j] = (_Float16)w;
     if constexpr (DT == 0) p.lo[j] = (_Float16)(w - (float)p.hi[j]);
   }

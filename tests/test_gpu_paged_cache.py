@@ -375,6 +375,53 @@ def test_attention_of_a_nan_reaches_its_row_and_channel_only():
     assert nan[0, :2, 10].all() and int(nan.sum()) == 2
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attention_whose_logits_are_so_large_that_a_difference_is_rounded(dtype):
+    """Logits near 2^25 are 4 apart in fp32.  Four pages of one, and four whose logits are 8.16 more, which fp32 takes for 8, in powers
+    of two: a maximum that lags may lag just as much, and m - 7 is rounded to m - 8.  Then logits of 2^20 to 2^26 of any kind."""
+    p = Pair(n_kv=1, G=2, max_seqs=2, max_ctx=1024, dtype=dtype)
+
+    def steep(x, gen):
+        x[0] = 0
+        x[0, :, :, 0] = 2.0 ** 14
+        x[0, 128:, :, 1] = 64
+        x[1] = torch.randn(x[1].shape, generator=gen)
+        return x
+
+    p.grow([0], [256], steep)
+    q = torch.zeros((1, 2, D), dtype=TYPES[dtype])
+    q[0, 0, 0], q[0, 0, 1] = 2.0 ** 14, 1
+    p.check_attention(0, [0], q=q)
+    p.grow([1], [999], lambda x, gen: x * 1000)
+    for scale in (10.0, 100.0, 1000.0):
+        p.check_attention(0, [1], scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("at", [5, 69])
+def test_a_key_or_query_that_is_not_finite_is_not_lost(dtype, at):
+    """In a full page (token 5) or the open one (69): a weight that is held to the largest one still tells it."""
+    def bad(x, gen):
+        if x.shape[1] > 5:
+            x[0, at, 1, 77] = math.nan
+        return x
+
+    p = Pair(n_kv=2, G=2, max_seqs=4, dtype=dtype)
+    p.grow([0, 1], [70, 70], bad)
+    p.c.free(ints([1]))
+    p.m.free([1])
+    p.grow([1], [70])
+    q = p.queries(4)
+    q[2, 1, 3] = math.nan
+    q[3, 2, 99] = math.inf
+    out = torch.empty_like(q, device="cuda")
+    p.c.attn(0, ints([0, 1, 1, 1]), q.cuda(), out)
+    nan = out.isnan().cpu()
+    want = torch.zeros((4, 4), dtype=torch.bool)
+    want[0, 2:] = want[2, 1] = want[3, 2] = True
+    assert torch.equal(nan, want[..., None].expand_as(nan))
+
+
 def test_open_pages_of_others_do_not_matter():
     """What a slot's open page held before -- here NaN -- is not seen behind its new tokens."""
     p = Pair(n_kv=1, G=2, max_seqs=1)
