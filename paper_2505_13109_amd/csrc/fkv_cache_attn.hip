@@ -1,6 +1,8 @@
 // Attention of one query token per row over the paged cache in 4 bits.
 #include "fkv_cache.h"
 
+#include <cfloat>
+
 namespace fkv {
 
 namespace {
@@ -344,7 +346,7 @@ struct Joined {
 template <int N>
 __device__ __forceinline__ void join(const unsigned long long* part, const unsigned long long* ml, size_t part_step, size_t ml_step, int count, Joined* r) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) r[j] = Joined{-1e30f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < N; ++j) r[j] = Joined{-FLT_MAX, 0.f, 0.f, 0.f};
   for (int k0 = 0; k0 < count; k0 += JOIN) {
     unsigned long long v[N][JOIN], w[N][JOIN];
 #pragma unroll
@@ -453,7 +455,7 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
   }
   const float scale = 0.08838834764831845f * 1.4426950408889634f;      // 1 / sqrt(128), in powers of two
   Seen seen;
-  seen.m = -1e30f;
+  seen.m = -FLT_MAX;
   seen.l = f32x4{0, 0, 0, 0};
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) seen.acc[cb] = f32x4{0, 0, 0, 0};

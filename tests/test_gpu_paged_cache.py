@@ -397,6 +397,21 @@ def test_attention_whose_logits_are_so_large_that_a_difference_is_rounded(dtype)
         p.check_attention(0, [1], scale=scale)
 
 
+def test_attention_whose_logits_are_far_below_zero():
+    """All of them the same, -2^113 or so: the weights are, too, and the output is what logits of zero give."""
+    p = Pair(n_kv=1, G=4, max_seqs=3, max_ctx=2048, n_pages=100)
+
+    def low(x, gen):
+        x[0] = -2.0 ** 50
+        return x
+
+    p.grow([0, 1, 2], [2000, 5, 70], low)
+    q = torch.full((3, 4, D), 2.0 ** 60, dtype=torch.bfloat16)
+    out = torch.zeros_like(q, device="cuda")
+    p.c.attn(0, ints([0, 1, 2]), q.cuda(), out)
+    p.check_attention(0, [0, 1, 2], q=torch.zeros_like(q), got=out.cpu())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("at", [5, 69])
 def test_a_key_or_query_that_is_not_finite_is_not_lost(dtype, at):
