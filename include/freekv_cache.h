@@ -18,9 +18,10 @@
  * A page of a KV head is 5120 bytes and an exponent, 16384 bytes in T.
  *
  * State lives on the device.  Lengths, page tables, reference counts and the free pages are in the arena, and the calls
- * below only enqueue kernels that read and change them: no call waits for the GPU, page ids never pass through the host, and
- * captured into a graph every replay does the work again on the state of that time.  What only the device can see to be wrong (a slot that does not exist, a pool without room) makes
- * no access: the entry, or the whole call where it says so, does nothing, and fkv_cache_health reports it.
+ * below only enqueue kernels that read and change them, but for those that say that they are blocking: page ids never pass through
+ * the host, and captured into a graph every replay does the work again on the state of that time.  What only the device can see
+ * to be wrong (a slot that does not exist, a pool without room) makes no access: the entry, or the whole call where it says so,
+ * does nothing, and fkv_cache_health reports it.
  *
  * Conventions are those of freekv.h: 0 or a negative FKV_E* code, fkv_cache_last_error for the text, `stream` a hipStream_t,
  * device pointers.  A call launches on the cache's device, whichever is current.  The calls on one cache (on either, for
@@ -60,6 +61,7 @@ int fkv_cache_arena_bytes(const fkv_cache_config* cfg, size_t* dev_bytes);
 /* An empty cache on the current device.  dev_arena: device memory, 256-byte aligned, >= dev_bytes; the caller's, to be kept
  * as long as the cache.  Blocking. */
 int fkv_cache_create(const fkv_cache_config* cfg, void* dev_arena, size_t dev_bytes, fkv_cache** out);
+/* Blocking: the arena may be freed behind it. */
 int fkv_cache_destroy(fkv_cache* cache);
 /* Text of the last error of this cache (cache == NULL: of this thread's last failed create or arena_bytes). */
 const char* fkv_cache_last_error(const fkv_cache* cache);

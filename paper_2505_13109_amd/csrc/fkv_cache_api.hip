@@ -177,6 +177,10 @@ int fkv_cache_create(const fkv_cache_config* cfg, void* dev_arena, size_t dev_by
 
 int fkv_cache_destroy(fkv_cache* c) {
   if (!c) return FKV_EINVAL;
+  {
+    OnDevice on_device(c);
+    (void)hipDeviceSynchronize();
+  }
   delete c;
   return FKV_OK;
 }

@@ -853,6 +853,20 @@ def test_on_a_stream_of_the_callers():
     p.check_attention(0, [1], q=q, got=out.cpu())
 
 
+def test_close_waits_for_what_is_still_running():
+    """The arena goes back to the allocator with the cache, whatever stream still reads it."""
+    p = Pair(n_kv=8, G=4, max_seqs=2, max_ctx=65536, n_pages=2100)
+    p.grow([0], [65536])
+    s = torch.cuda.Stream()
+    q, seqs = p.queries(1).cuda(), ints([0])
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    for _ in range(200):
+        p.c.attn(0, seqs, q, out, stream=s)
+    p.c.close()
+    assert s.query()
+
+
 def test_two_caches_at_once_on_two_streams():
     a, b = (Pair(n_kv=2, G=4, max_seqs=2, max_ctx=8192, n_pages=300, seed=i) for i in (1, 2))
     for p in (a, b):
