@@ -53,7 +53,7 @@ typedef struct {
   int32_t max_ctx;         /* most tokens of a sequence, a multiple of page_size    */
   int32_t n_pages;         /* pages of the pool                                     */
   int32_t dtype;           /* FKV_DTYPE_*: of q, K, V and the outputs                */
-} fkv_cache_config;
+} fkv_cache_config;        /* n_layers * max_seqs * n_kv_heads: at most 8388608      */
 
 /* Bytes of device memory that such a cache needs: the pool, 16 KiB per layer, slot and KV head for open pages, tables,
  * and the workspace of attention. */

@@ -24,7 +24,8 @@ const char* check_config(const fkv_cache_config* c) {
   if (c->n_q_heads < c->n_kv_heads || c->n_q_heads % c->n_kv_heads) return "n_q_heads must be a multiple of n_kv_heads";
   if (c->n_q_heads / c->n_kv_heads > CACHE_MAX_G) return "group size above 16 is not supported";
   if (c->max_seqs < 1 || c->max_seqs > CACHE_MAX_SEQS) return "max_seqs must be 1 to 4096";
-  if ((size_t)c->n_layers * c->max_seqs * c->n_kv_heads > (1u << 25)) return "more than 33554432 open pages (layers x slots x KV heads) are not supported";
+  // (a copy has a block of 256 threads for each of them, and some more, and a launch fewer than 2^32 threads)
+  if ((size_t)c->n_layers * c->max_seqs * c->n_kv_heads > (1u << 23)) return "more than 8388608 open pages (layers x slots x KV heads) are not supported";
   if (c->max_ctx < PG || c->max_ctx % PG || c->max_ctx > (1 << 22)) return "max_ctx must be a multiple of page_size, at most 4194304";
   if (c->n_pages < 1 || c->n_pages > (1 << 26)) return "n_pages must be 1 to 67108864";
   if (c->dtype != FKV_DTYPE_FP16 && c->dtype != FKV_DTYPE_BF16) return "dtype must be fp16 or bf16";

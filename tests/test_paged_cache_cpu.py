@@ -31,6 +31,16 @@ def test_arena_and_config():
     assert L.fkv_cache_arena_bytes(None, C.byref(need)) == -1
 
 
+def test_as_many_open_pages_as_a_copy_has_blocks_for():
+    L = fkv.lib()
+    need = C.c_size_t()
+    assert L.fkv_cache_arena_bytes(C.byref(_cfg(n_layers=256, max_seqs=4096, n_kv_heads=8)), C.byref(need)) == 0 and need.value > 2 ** 37
+    assert (256 * 4096 * 8 + 2 ** 20) * 256 < 2 ** 32
+    for more in (dict(n_layers=257, max_seqs=4096), dict(n_layers=512, max_seqs=4096), dict(n_layers=4096, max_seqs=4096, n_kv_heads=1, n_q_heads=1)):
+        assert L.fkv_cache_arena_bytes(C.byref(_cfg(**more)), C.byref(need)) == -1, more
+        assert b"open pages" in L.fkv_cache_last_error(None)
+
+
 def test_create_refuses_bad_arenas_without_touching_the_gpu():
     L = fkv.lib()
     h = C.c_void_p()
