@@ -130,7 +130,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_extend_kernel(CacheDesc c,
     if (j >= per || i >= n_rows) continue;
     const int s = seqs[i];
     const int m = cu ? max(cu[i], 0) : 0;
-    const int t = cu ? cu[i + 1] - m : 1;
+    const int t = !cu ? 1 : cu[i + 1] < m ? -1 : cu[i + 1] - m;
     if (s == -1) continue;
     if (s < 0 || s >= c.max_seqs || first[s] != i || t < 0) { faults |= FAULT_ENTRY; continue; }
     slot[j] = s;

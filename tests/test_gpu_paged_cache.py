@@ -508,6 +508,36 @@ def test_compact_and_copy_keep_what_sequences_hold():
     p.check_tables()
 
 
+def test_compact_between_an_extend_and_its_appends():
+    """New pages move before they are filled, in one layer or in all; tokens still come once."""
+    p = Pair(n_layers=3, n_kv=2, max_seqs=4, max_ctx=512, n_pages=40)
+    p.grow([0, 1, 2], [200, 70, 100])
+    p.c.free(ints([0]))
+    p.m.free([0])
+    p.c.compact()                                        # (pages that are free now have been used)
+    p.m.compact()
+    p.grow([3], [128])
+    p.c.free(ints([1]))
+    p.m.free([1])
+    seqs, new, cu = [2, 3], [75, 40], offsets([75, 40])
+    p.c.extend(ints(seqs), cu)
+    assert p.m.extend(seqs, new)
+    for layer in range(3):
+        k, v = tokens(p.gen, sum(new), 2, "bf16")
+        p.c.append(layer, ints(seqs), k.cuda(), v.cuda(), cu)
+        p.m.append(layer, seqs, new, k, v)
+        if layer == 0:
+            p.c.compact()
+            p.m.compact()
+    p.check_tables()
+    p.check_contents()
+    other = torch.full((sum(new), 2, D), 9.0, dtype=torch.bfloat16, device="cuda")
+    for layer in range(3):
+        p.c.append(layer, ints(seqs), other, other, cu)
+    _refused(p, "passed over")
+    p.check_contents()
+
+
 @pytest.mark.parametrize("seed", range(4))
 def test_any_order_of_operations(seed):
     """A run of them as a scheduler would make it, small pool, against the model."""
@@ -722,6 +752,15 @@ def test_token_offsets_that_make_no_sense_reach_nothing():
         p.c.health()
     p.check_tables()
     p.check_contents()
+
+
+def test_an_extend_whose_token_offsets_fall_refuses_the_row():
+    p = Pair(n_kv=1, max_seqs=4, max_ctx=256, n_pages=32)
+    p.grow([0], [40])
+    for cu in ([5, 4], [2 ** 31 - 1, -2 ** 31], [2 ** 31 - 1, 0], [3, -5]):
+        p.c.extend(ints([0]), ints(cu))
+        _refused(p, "passed over")
+    p.check_tables()
 
 
 def test_arguments_are_refused_before_a_launch():
