@@ -31,7 +31,7 @@ __device__ __forceinline__ half8 key_codes(uint32_t w) {
 // 2^-15 of their sum on the way, and an output over 128K tokens, small among its values, came out 0.4 % off.
 // 64 + code takes seven instructions and leaves 1e-4 of such an output, for bf16; 16 + code takes eight, for fp16.
 // (The base's bits come from a register that is not known to be a constant: an instruction takes one constant, and masking and
-// setting are one of three operands so, 32 fewer to a page, 373 -> 341.)
+// setting are one of three operands so: 32 fewer to a page, which takes some 350.)
 template <int DT> constexpr float VALUE_BASE = DT ? 64.f : 16.f;
 template <int DT> __device__ __forceinline__ uint32_t value_bits() {
   uint32_t b = DT ? 0x54005400u : 0x4c004c00u;

@@ -508,6 +508,47 @@ def test_compact_and_copy_keep_what_sequences_hold():
     p.check_tables()
 
 
+def test_copy_between_caches_of_other_sizes():
+    """From slots that the target does not have, more entries than the source has slots, a sequence too long for the target; on a
+    stream of the caller's, captured, with the target emptied between the replays."""
+    a = Pair(n_layers=2, n_kv=2, G=1, max_seqs=9, max_ctx=512, n_pages=64)
+    b = Pair(n_layers=2, n_kv=2, G=4, max_seqs=3, max_ctx=128, n_pages=9)
+    c = Pair(n_layers=2, n_kv=2, G=2, max_seqs=12, max_ctx=256, n_pages=64)
+    a.grow([8, 2, 5], [100, 300, 31])
+    b.grow([1], [64])
+    src, dst = [8, 2], [2, 0]
+
+    def step(stream=None):
+        a.c.copy(ints_src, ints_dst, to=b.c, stream=stream)
+
+    ints_src, ints_dst = ints(src), ints(dst)
+    step()
+    a.m.copy([8], [2], to=b.m)
+    _refused(b, "max_ctx")
+    a.c.health()
+    b.check_tables()
+    b.check_contents()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    b.c.free(ints([2]))
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for i in range(3):
+        graph.replay()
+        _refused(b, "max_ctx")
+        b.check_tables()
+        b.check_contents()
+        if i < 2:
+            b.c.free(ints([2]))
+    # every slot of a larger one from two of a smaller one
+    many = [1, 2] * 6
+    assert b.m.copy(many, list(range(12)), to=c.m)
+    b.c.copy(ints(many), ints(list(range(12))), to=c.c)
+    c.check_tables()
+    c.check_contents()
+    c.check_attention(1, list(range(12)))
+
+
 def test_compact_between_an_extend_and_its_appends():
     """New pages move before they are filled, in one layer or in all; tokens still come once."""
     p = Pair(n_layers=3, n_kv=2, max_seqs=4, max_ctx=512, n_pages=40)
