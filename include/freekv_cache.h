@@ -94,6 +94,8 @@ int fkv_cache_append(fkv_cache* cache, int32_t layer, const int32_t* seqs_dev, i
  *              last window_tokens tokens' full pages (both multiples of page_size, the sink first if they overlap) and the
  *              open page, which are attended always.  Entries that are not a full page between sink and window
  *              (-1, say) are passed over; one that is listed twice counts twice.  n_list: 0 to 131072.
+ * Branches among up to 64 rows of a call with G <= 8 read the pages that they shared at their last fork together, whatever the
+ * rows' order.
  * Softmax and sums are in fp32, the output is rounded once.  A row that has nothing to attend (padding, an empty sequence,
  * an empty list) gets zeros. */
 int fkv_cache_attn(fkv_cache* cache, int32_t layer, const int32_t* seqs_dev, int32_t n_rows, const void* q_dev,

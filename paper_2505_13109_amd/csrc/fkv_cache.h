@@ -46,6 +46,7 @@ struct CacheDesc {
   int32_t* owner;        // [slot] its row, and
   int32_t* serial;       // [slot] its number, which
   int32_t* appended;     // [layer][slot][n_kv] takes over when the first of its tokens are there
+  int32_t* kin;          // [slot] pages that it shared at its last fork, from it or into it
   int32_t* table;        // [slot][max_pages] page ids
   int32_t* ref;          // [page] sequences that share it
   int32_t* uses;         // [page] how often it has been taken from the pool
@@ -54,8 +55,8 @@ struct CacheDesc {
   int32_t* to;           //        to page
   int32_t* remap;        // [page] new number of a page that moved
   int32_t* ok;           // [slot] fork, copy: the source of entry i, -1: nothing to do
-  unsigned long long* part;      // attention: a split's sums, pairs of channels, [item][n_kv][G][d / 2], and
-  unsigned long long* part_ml;   // [item][n_kv][G] its maximum and sum of weights
+  unsigned long long* part;      // attention: a split's sums, pairs of channels, [item][n_kv][heads][d / 2], and
+  unsigned long long* part_ml;   // [item][n_kv][heads] its maximum and sum of weights
   unsigned long long* group_ml;  // the same of a group of splits, at its first one
   int32_t* ticket;       // [row][n_kv][CACHE_TICKETS] splits that are done: of all groups, and of each group
   int n_layers, n_kv, G, max_seqs, max_pages, n_pages, dtype;
@@ -67,6 +68,9 @@ struct CacheDesc {
 // Blocks that attention is cut into, about: two of four waves for each of 256 compute units.
 constexpr int CACHE_ATTN_BLOCKS = 512;
 inline int cache_attn_items(int n_rows, int n_kv) { return CACHE_ATTN_BLOCKS / n_kv + n_rows + 1; }
+// Rows among which branches are looked for, one to a lane; the heads of as many as are taken together.
+constexpr int CACHE_KIN_ROWS = 64;
+__host__ __device__ inline int cache_attn_heads(int G) { return CACHE_MAX_G / G * G; }
 
 void launch_cache_extend(const CacheDesc& c, const int32_t* seqs, int n_rows, const int32_t* cu, hipStream_t st);
 void launch_cache_append(const CacheDesc& c, int layer, const int32_t* seqs, int n_rows, const int32_t* cu, const uint16_t* k, const uint16_t* v,
@@ -80,7 +84,8 @@ struct CacheAttn {
   uint16_t* out;
   int layer, n_rows, n_list, n_sink, n_win;
 };
-void launch_cache_attn(const CacheDesc& c, const CacheAttn& a, hipStream_t st);
+// forked: whether there has been a fork, so that rows may share pages
+void launch_cache_attn(const CacheDesc& c, const CacheAttn& a, bool forked, hipStream_t st);
 void launch_cache_fork(const CacheDesc& c, const int32_t* src, const int32_t* dst, int n, hipStream_t st);
 void launch_cache_copy(const CacheDesc& from, const int32_t* src, const CacheDesc& to, const int32_t* dst, int n, hipStream_t st);
 void launch_cache_free(const CacheDesc& c, const int32_t* seqs, int n, hipStream_t st);

@@ -2,6 +2,7 @@
 #include "../../include/freekv_cache.h"
 #include "fkv_cache.h"
 
+#include <algorithm>
 #include <cstdio>
 #include <new>
 #include <type_traits>
@@ -38,7 +39,8 @@ size_t lay_out(const fkv_cache_config& c, char* base, CacheDesc* d) {
   x.n_layers = c.n_layers; x.n_kv = c.n_kv_heads; x.G = c.n_q_heads / c.n_kv_heads; x.max_seqs = c.max_seqs;
   x.max_pages = c.max_ctx / PG; x.n_pages = c.n_pages; x.dtype = c.dtype;
   const size_t units = (size_t)c.n_layers * c.n_pages * c.n_kv_heads, opens = (size_t)c.n_layers * c.max_seqs * c.n_kv_heads;
-  const size_t items = (size_t)cache_attn_items(c.max_seqs, c.n_kv_heads) * c.n_kv_heads;
+  auto slabs = [&](int rows) { return (size_t)cache_attn_items(rows, c.n_kv_heads) * c.n_kv_heads; };
+  const size_t heads = std::max(slabs(std::min(c.max_seqs, CACHE_KIN_ROWS)) * cache_attn_heads(x.G), slabs(c.max_seqs) * x.G);
   size_t at = 0;
   auto take = [&](auto*& p, size_t bytes) {
     p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(reinterpret_cast<uintptr_t>(base) + at);
@@ -56,14 +58,15 @@ size_t lay_out(const fkv_cache_config& c, char* base, CacheDesc* d) {
   take(x.info, units * 4);
   take(x.used, (size_t)(c.n_pages + 31) / 32 * 4);
   take(x.ticket, (size_t)c.max_seqs * c.n_kv_heads * CACHE_TICKETS * 4);
+  take(x.kin, (size_t)c.max_seqs * 4);
   take(x.table, (size_t)c.max_seqs * x.max_pages * 4);
   take(x.from, (size_t)c.n_pages * 4);
   take(x.to, (size_t)c.n_pages * 4);
   take(x.remap, (size_t)c.n_pages * 4);
   take(x.ok, (size_t)c.max_seqs * 4);
-  take(x.part_ml, items * x.G * 8);
-  take(x.group_ml, items * x.G * 8);
-  take(x.part, items * x.G * D * 4);
+  take(x.part_ml, heads * 8);
+  take(x.group_ml, heads * 8);
+  take(x.part, heads * D * 4);
   take(x.open, opens * OPEN_ELEMS * 2);
   take(x.units, units * CU_BYTES);
   if (d) *d = x;
@@ -76,6 +79,7 @@ struct fkv_cache {
   fkv_cache_config cfg;
   CacheDesc desc;
   int device;
+  bool forked;
   char err[ERR];
 
   int fail(int code, const char* what) {
@@ -253,7 +257,7 @@ int fkv_cache_attn(fkv_cache* c, int32_t layer, const int32_t* seqs, int32_t n_r
   a.pages = pages;
   a.out = static_cast<uint16_t*>(out);
   a.layer = layer; a.n_rows = n_rows; a.n_list = n_list; a.n_sink = sink_tokens / PG; a.n_win = window_tokens / PG;
-  launch_cache_attn(c->desc, a, static_cast<hipStream_t>(stream));
+  launch_cache_attn(c->desc, a, c->forked, static_cast<hipStream_t>(stream));
   return after_launch(c, "attention kernel");
 }
 
@@ -261,6 +265,7 @@ int fkv_cache_fork(fkv_cache* c, const int32_t* src, const int32_t* dst, int32_t
   FKV_CACHE(c);
   FKV_ROWS(check_rows(c, src, n));
   FKV_ROWS(check_rows(c, dst, n));
+  c->forked = true;
   launch_cache_fork(c->desc, src, dst, n, static_cast<hipStream_t>(stream));
   return after_launch(c, "fork kernels");
 }

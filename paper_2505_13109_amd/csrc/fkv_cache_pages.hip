@@ -238,6 +238,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_fork_kernel(CacheDesc a, c
     c.ok[i] = room ? s[j] : -1;
     if (s[j] < 0 || !room) continue;
     c.len[d[j]] = len[j];
+    if (!COPY && len[j] >= PG) c.kin[d[j]] = c.kin[s[j]] = len[j] / PG;
     c.added[d[j]] = 0;
     c.owner[d[j]] = -1;
   }
@@ -412,6 +413,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_free_kernel(CacheDesc c, c
   if (threadIdx.x == 0) {
     if (freed) atomicSub(&c.head[CACHE_USED], freed);
     c.len[s] = 0;
+    c.kin[s] = 0;
     c.added[s] = 0;
     c.owner[s] = -1;
   }

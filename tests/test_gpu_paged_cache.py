@@ -347,6 +347,138 @@ def test_as_many_slots_as_there_may_be():
     p.check_tables()
 
 
+def branches(p, shape, seed=0):
+    """Sequences of `shape` = [(tokens of a prompt, [tokens of a branch behind it, ..]), ..] in slots 0, 1, ..; returns their numbers."""
+    slots, at = [], 0
+    for prompt, tails in shape:
+        first = at
+        p.grow([first], [prompt])
+        rest = list(range(first + 1, first + len(tails)))
+        if rest:
+            p.c.fork(ints([first] * len(rest)), ints(rest))
+            p.m.fork([first] * len(rest), rest)
+        for s, n in zip(range(first, first + len(tails)), tails):
+            if n:
+                p.grow([s], [n])
+        at += len(tails)
+        slots += range(first, at)
+    return slots
+
+
+@pytest.mark.parametrize("kv,G,dtype", [(32, 1, "bf16"), (32, 3, "fp16"), (32, 4, "bf16"), (40, 7, "bf16"), (32, 8, "fp16"), (32, 11, "bf16")])
+def test_attention_of_branches(kv, G, dtype):
+    """Rows that share pages are taken together where there are many pages to a KV head: more of a kind than fit together, tails of none
+    to more pages than are shared, open pages or none, in an order that mixes them with others, twice, and with padding."""
+    p = Pair(n_kv=kv, G=G, max_seqs=24, max_ctx=1536, n_pages=220, dtype=dtype)
+    slots = branches(p, [(500, [0, 1, 12, 12 + 32, 200, 33]), (288, [0, 0, 32]), (700, [0]), (260, [5, 600])])
+    p.grow([20], [320])
+    slots += [20]
+    rng = random.Random(kv + G)
+    for k in range(2):
+        rng.shuffle(slots)
+        rows = slots[:7] + [-1] + slots[7:] + [slots[3], 23]
+        p.check_attention(0, rows)
+    p.c.free(ints([0, 6]))                               # the prompts' own slots: branches share on
+    p.m.free([0, 6])
+    p.c.compact()
+    p.m.compact()
+    p.check_tables()
+    p.check_attention(0, slots)
+    # branches of branches, and slots that others use now
+    p.c.fork(ints([4, 4, 11]), ints([0, 21, 22]))
+    p.m.fork([4, 4, 11], [0, 21, 22])
+    p.grow([0, 4, 6, 22], [40, 64, 290, 1])
+    p.check_attention(0, slots + [21, 22])
+
+
+def test_attention_of_many_branches_in_many_splits():
+    """One KV head, 64 rows of 8 prompts; splits of several levels, and none of the rows' pages shared in the end."""
+    p = Pair(n_kv=2, G=2, max_seqs=66, max_ctx=4096, n_pages=1200)
+    branches(p, [(n, [1 + (n + i) % 70 for i in range(8)]) for n in (3900, 64, 300, 2000, 1024, 31, 999, 3000)])
+    order = list(range(64))
+    random.Random(3).shuffle(order)
+    p.check_attention(0, order)
+    p.check_attention(0, order[:33])
+    p.c.copy(ints(order[:1]), ints([64]))
+    assert p.m.copy(order[:1], [64])
+    p.check_attention(0, order[:63] + [64])
+    p.check_attention(0, list(range(65)))                # (more rows than a wave has lanes: each by itself)
+
+
+def test_branches_decode_in_a_graph():
+    """Captured while two prompts' branches are apart by nothing: replays go on through full pages, a compaction and other branches."""
+    p = Pair(n_kv=32, G=4, max_seqs=9, max_ctx=1536, n_pages=200)
+    p.grow([0, 4], [1000, 831])
+    p.c.fork(ints([0, 0, 0, 4]), ints([1, 2, 3, 5]))
+    p.m.fork([0, 0, 0, 4], [1, 2, 3, 5])
+    rows = [5, 0, 2, 4, 1, 3]
+    seqs, q = ints(rows), p.queries(6)
+    k, v = tokens(p.gen, 6, 32, "bf16")
+    kd, vd, qd = k.cuda(), v.cuda(), q.cuda()
+    out = torch.empty_like(qd)
+
+    def step():
+        p.c.extend(seqs)
+        p.c.append(0, seqs, kd, vd)
+        p.c.attn(0, seqs, qd, out)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(30):
+        k, v = tokens(p.gen, 6, 32, "bf16")
+        kd.copy_(k), vd.copy_(v)
+        graph.replay()
+        assert p.m.extend(rows, [1] * 6)
+        p.m.append(0, rows, [1] * 6, k, v)
+        if i in (0, 8, 23, 24, 25, 29):
+            p.check_attention(0, rows, q=q, got=out.cpu())
+        if i == 8:                                       # slot 3 becomes a branch of slot 1
+            p.c.free(ints([3]))
+            p.m.free([3])
+            p.c.compact()
+            p.m.compact()
+            p.c.fork(ints([1]), ints([3]))
+            p.m.fork([1], [3])
+    p.check_tables()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("at", ["a key", "a value", "an open key", "an open value", "a query"])
+def test_a_branch_that_is_not_finite_leaves_the_others_alone(at, dtype):
+    p = Pair(n_kv=32, G=2, max_seqs=6, max_ctx=1024, n_pages=100, dtype=dtype)
+    p.grow([0], [700])
+    p.c.fork(ints([0] * 4), ints([1, 2, 3, 4]))
+    p.m.fork([0] * 4, [1, 2, 3, 4])
+    p.grow([0, 1, 3, 4], [70, 1, 40, 99])
+    q = p.queries(5)
+    clean = torch.empty_like(q, device="cuda")
+    bad = torch.empty_like(clean)
+    rows = ints([0, 1, 2, 3, 4])
+
+    def worse(x, gen):
+        x[0 if "key" in at else 1] = math.nan
+        return x
+
+    p.grow([2], [100 if "open" not in at else 5])
+    p.c.attn(0, rows, q.cuda(), clean)
+    p.c.free(ints([2]))
+    p.c.fork(ints([1]), ints([2]))                       # (698 tokens' pages are those of the others still)
+    p.m.free([2])
+    p.m.fork([1], [2])
+    if at == "a query":
+        q[2] = math.nan
+        p.grow([2], [100])
+    else:
+        p.grow([2], [100 if "open" not in at else 5], worse)
+    p.c.attn(0, rows, q.cuda(), bad)
+    others = [0, 1, 3, 4]
+    assert bad[2].isnan().all()
+    p.check_attention(0, others, q=q[others], got=bad.cpu()[others])
+    p.check_attention(0, others, q=q[others], got=clean.cpu()[others])
+
+
 def test_attention_is_the_same_every_time():
     """Splits are joined in their order whichever ends last."""
     p = Pair(n_kv=2, G=4, max_seqs=3, max_ctx=8192, n_pages=600)
