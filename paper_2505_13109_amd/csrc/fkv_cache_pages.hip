@@ -322,44 +322,30 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheDesc a, CacheDesc 
   }
 }
 
-// One block: used pages behind the first `pages in use` go to the free places before that, in order.
+// One block: used pages behind the first `pages in use` go to the free places before that, in order.  Both are counted in one pass, 16 bits
+// each: a thousand words have 32768 pages.
 __global__ __launch_bounds__(PLAN_THREADS) void cache_compact_kernel(CacheDesc c) {
   __shared__ int sh[PLAN_THREADS / 64];
   const int live = c.head[CACHE_USED], words = (c.n_pages + 31) / 32;
-  int holes = 0;
-  for (int w0 = 0; w0 < (live + 31) / 32; w0 += PLAN_THREADS) {
+  int holes = 0, moved = 0;
+  for (int w0 = 0; w0 < words; w0 += PLAN_THREADS) {
     const int w = w0 + (int)threadIdx.x;
-    uint32_t bits = 0;
-    if (w * 32 < live) {
-      bits = ~c.used[w];
-      if (live - w * 32 < 32) bits &= (1u << (live - w * 32)) - 1;
-    }
-    int here;
-    int k = holes + scan_block(__popc(bits), &here, sh);
-    for (; bits; bits &= bits - 1, ++k) c.to[k] = w * 32 + __ffs((int)bits) - 1;
-    holes += here;
+    const uint32_t used = w < words ? c.used[w] : 0;
+    const int below = min(max(live - w * 32, 0), 32);      // this word's pages that will be the ones in use
+    const uint32_t first = below == 32 ? ~0u : (1u << below) - 1;
+    uint32_t free_bits = ~used & first, tail = used & ~first;
+    int both;
+    const uint32_t before = (uint32_t)scan_block((int)(__popc(free_bits) | (uint32_t)__popc(tail) << 16), &both, sh);
+    int k = holes + (int)(before & 0xffff);
+    for (; free_bits; free_bits &= free_bits - 1, ++k) c.to[k] = w * 32 + __ffs((int)free_bits) - 1;
+    k = moved + (int)(before >> 16);
+    for (; tail; tail &= tail - 1, ++k) c.from[k] = w * 32 + __ffs((int)tail) - 1;
+    if (w < words && used != first) c.used[w] = first;
+    holes += both & 0xffff;
+    moved += (int)((uint32_t)both >> 16);
   }
   __syncthreads();
-  int moved = 0;
-  for (int w0 = live / 32; w0 < words; w0 += PLAN_THREADS) {
-    const int w = w0 + (int)threadIdx.x;
-    uint32_t bits = 0;
-    if (w < words) {
-      bits = c.used[w];
-      if (w * 32 < live) bits &= ~((1u << (live - w * 32)) - 1);
-    }
-    int here;
-    int k = moved + scan_block(__popc(bits), &here, sh);
-    for (; bits; bits &= bits - 1, ++k) {
-      const int page = w * 32 + __ffs((int)bits) - 1;
-      c.from[k] = page;
-      c.remap[page] = c.to[k];
-    }
-    moved += here;
-  }
-  __syncthreads();
-  for (int w = threadIdx.x; w < words; w += PLAN_THREADS)
-    c.used[w] = w * 32 >= live ? 0u : live - w * 32 >= 32 ? ~0u : (1u << (live - w * 32)) - 1;
+  for (int k = threadIdx.x; k < moved; k += PLAN_THREADS) c.remap[c.from[k]] = c.to[k];
   if (threadIdx.x == 0) c.head[CACHE_MOVES] = moved;
 }
 
