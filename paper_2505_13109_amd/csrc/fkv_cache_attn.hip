@@ -112,18 +112,49 @@ __device__ __forceinline__ void raise(Seen& s, float top, int lane) {
   for (int cb = 0; cb < 8; ++cb) s.acc[cb] *= g;
 }
 
-// A full page's keys: x = q (lo + step code).  The product of q and step is made here, per page and channel, in two fp16 halves
-// (exact: 8 or 11 bits times 11); the codes are the other operand.  x[mb][i] is head n's, token mb 16 + kb 4 + i's part of the codes;
-// f x + b is the logit in powers of two.
+// A full page's keys: x = q (lo + step code).  The product of q and step is made here, per page and channel, in two fp16 halves; the
+// codes are the other operand.  x[mb][i] is head n's, token mb 16 + kb 4 + i's part of the codes; f x + b is the logit in powers of two.
+//
+// The halves are of q16 step, q16 = q 2^(13 - q_exp) being a head's queries in fp16 with the largest one at 2^13 to 2^14: together they hold what is
+// above 2^-25, where a largest query that meets the page's largest step gives 2^15.  But the two need not belong to one channel.  Products that count may be
+// far below, where a query's large channels meet keys that hardly change in them.  A logit loses up to 128 channels x code 15 x 3 x 2^-25 (a
+// rounding of q16 times a step of up to 2, and one of the low half), 2^(E + q_exp - 29) with the powers of two and 1 / sqrt(128): 2^-17 where they
+// add up to WIDE.  Beyond, the halves are of each page's products relative to the largest of them: 128K x 4 tokens take
+// 213 us where all pages are such instead of 122.
+constexpr int WIDE = 12;
+
+// Eight channels in fp32, not known to the compiler to be the same for every page: it would keep all of them in registers.
+template <int DT> __device__ __forceinline__ void queries(u32x4 w, float* q) {
+  asm volatile("" : "+v"(w));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = (i & 1) ? Unpack<DT>::hi(w[i >> 1]) : Unpack<DT>::lo(w[i >> 1]);
+}
+// floor(log2) + 1 of the largest product of query and step of this lane's head, 0 if there is none.  (Powers of two are added as whole
+// numbers: q goes down to T's smallest number, a page's steps over 2^-24 to 2.)
+template <int DT>
+__device__ __forceinline__ int largest_product(const Keys& r, const u32x4* qT) {
+  constexpr int NONE = -1000;
+  int top = NONE;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float q[8];
+    queries<DT>(qT[j], q);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float step = (float)__builtin_bit_cast(half8, r.step[j])[i];
+      top = max(top, q[i] != 0.f && step != 0.f ? __builtin_amdgcn_frexp_expf(q[i]) + __builtin_amdgcn_frexp_expf(step) : NONE);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  top = (int)max_groups((float)top);
+  return top == NONE ? 0 : top;
+}
+
 template <int DT>
 __device__ __forceinline__ void page_logits(const Keys& r, const half8* q16, const u32x4* qT, int q_exp, float scale, f32x4* x, float* f, float* b) {
   f32x4 bias = {0, 0, 0, 0};
   x[0] = x[1] = bias;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const half8 step = __builtin_bit_cast(half8, r.step[j]);
-    const half8 hi = q16[j] * step;
-    const half8 lo = __builtin_elementwise_fma(q16[j], step, -hi);
+  auto add = [&](int j, half8 hi, half8 lo) {
     const uint32_t w0 = j == 0 ? r.k[0].x : j == 1 ? r.k[0].y : j == 2 ? r.k[0].z : r.k[0].w;
     const uint32_t w1 = j == 0 ? r.k[1].x : j == 1 ? r.k[1].y : j == 2 ? r.k[1].z : r.k[1].w;
     const half8 a0 = key_codes(w0), a1 = key_codes(w1);
@@ -132,8 +163,41 @@ __device__ __forceinline__ void page_logits(const Keys& r, const half8* q16, con
     x[0] = mfma_h(a0, lo, x[0]);
     x[1] = mfma_h(a1, lo, x[1]);
     bias = mfma_T<DT>(__builtin_bit_cast(u32x4, r.lo[j]), qT[j], bias);
+  };
+  int e = exp_of_keys(r.info) + q_exp;
+  if (__builtin_expect(!__any(e > WIDE), 1)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const half8 step = __builtin_bit_cast(half8, r.step[j]), hi = q16[j] * step;
+      add(j, hi, __builtin_elementwise_fma(q16[j], step, -hi));
+    }
+    e += 20 - 13;
+  } else {
+    const int P = largest_product<DT>(r, qT);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float q[8];
+      queries<DT>(qT[j], q);
+      half8 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // exact, at most 2^15; where the step is 0 the query may be of any size (one that is not finite tells by `bias`)
+        const float t = __builtin_amdgcn_fmed3f(ldexpf(q[i], 15 - P), -0x1p100f, 0x1p100f) * (float)__builtin_bit_cast(half8, r.step[j])[i];
+        hi[i] = (_Float16)t;
+        lo[i] = (_Float16)(t - (float)hi[i]);
+      }
+      add(j, hi, lo);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    e = exp_of_keys(r.info) + P + 20 - 15;
+    const int over = max(e - 120, 0);      // (a logit may be within fp32's range where 2^e is not)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[0][i] = ldexpf(x[0][i], over);
+      x[1][i] = ldexpf(x[1][i], over);
+    }
+    e -= over;
   }
-  const int e = min(max(exp_of_keys(r.info) + q_exp, -140), 126);
   *f = ldexpf(scale, e);
   *b = bias[0] * scale;
 }
@@ -592,7 +656,7 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(Unpack<DT>::lo(qT[j][i])), fabsf(Unpack<DT>::hi(qT[j][i]))));
     top = max_groups(top);
-    q_exp = top > 0.f && top < INFINITY ? max(ilogbf(top), -126) : 0;
+    q_exp = top < INFINITY ? max(ilogbf(top), -126) : 0;      // (ilogb of 0 is far below)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -601,7 +665,6 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
         q16[j][2 * i] = (_Float16)ldexpf(Unpack<DT>::lo(qT[j][i]), e);
         q16[j][2 * i + 1] = (_Float16)ldexpf(Unpack<DT>::hi(qT[j][i]), e);
       }
-    q_exp += 20 - 13;                                      // (and codes are in units of 2^-20)
   }
 
   // -- the pages

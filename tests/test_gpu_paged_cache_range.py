@@ -1,0 +1,63 @@
+"""The paged cache's attention at the ends of what the types hold, against the same model in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from paged_model import D
+from test_gpu_paged_cache import TYPES, Pair, ints
+
+pytestmark = pytest.mark.gpu
+
+
+def dead(channel, at=0.0):
+    """keys that hold the same number at every token of one channel"""
+    def make(x, gen):
+        x[0, ..., channel] = at
+        return x
+    return make
+
+
+@pytest.mark.parametrize("dtype,powers", [("bf16", (8, 12, 13, 16, 24, 27, 30, 40, 70, 120)), ("fp16", (8, 11, 13, 15))])
+@pytest.mark.parametrize("at", [0.0, 2.0 ** -13])
+def test_a_querys_largest_channel_may_meet_keys_that_do_not_change(dtype, powers, at):
+    """Its product counts for nothing, or the same at every token: what decides is 2^r below.  With heads beside it that have no such
+    channel, in a page alone, in many, and in the open one."""
+    p = Pair(n_kv=2, G=4, max_seqs=3, max_ctx=512, n_pages=40, dtype=dtype)
+    p.grow([0, 1, 2], [32, 460, 37], dead(0, at))
+    for r in powers:
+        q = p.queries(3)
+        q[:, 1::2, 0] = 2.0 ** r
+        q[:, 5, 0] = -2.0 ** r
+        if at:                                           # a logit that all share may be as large as fp32 still tells the others' differences
+            q[:, :, 0] = q[:, :, 0].clamp(-2.0 ** 15, 2.0 ** 15)
+        p.check_attention(0, [0, 1, 2], q=q)
+
+
+@pytest.mark.parametrize("dtype,span", [("bf16", 20), ("bf16", 40), ("fp16", 10)])
+def test_queries_and_keys_whose_channels_span_much(dtype, span):
+    """Channels of queries 2^-span to 2^span, of keys the other way round, and a page of keys that are all of one size behind them."""
+    p = Pair(n_kv=1, G=5, max_seqs=2, max_ctx=512, n_pages=40, dtype=dtype)
+    e = torch.linspace(-span, span, D).round()
+    low = -14 if dtype == "fp16" else -200
+    for shuffled in range(2):
+        s = shuffled
+        p.grow([s], [200], lambda x, gen: torch.stack((x[0] * torch.exp2((-e).clamp(min=low)), x[1])))
+        q = (torch.randn((1, 5, D), generator=p.gen) * torch.exp2(e)).to(TYPES[dtype])
+        p.check_attention(0, [s], q=q)
+        p.grow([s], [100], lambda x, gen: x * 2.0 ** -span)
+        p.check_attention(0, [s], q=q)
+        e = e[torch.randperm(D, generator=p.gen)]
+
+
+def test_branches_with_wide_queries():
+    """The same where branches are read together: one row's large channel changes nothing for the others."""
+    p = Pair(n_kv=32, G=2, max_seqs=6, max_ctx=1536, n_pages=100)
+    p.grow([0], [1300], dead(5))
+    p.c.fork(ints([0] * 4), ints([1, 2, 3, 4]))
+    p.m.fork([0] * 4, [1, 2, 3, 4])
+    p.grow([0, 1, 3, 4], [70, 1, 40, 99], dead(5))
+    q = p.queries(5)
+    q[2, ::3, 5] = 2.0 ** 45
+    q[4, :, 5] = -2.0 ** 33
+    p.check_attention(0, [0, 1, 2, 3, 4], q=q)
