@@ -81,10 +81,10 @@ __device__ __forceinline__ void load_values(const CacheDesc& c, size_t u, int la
 }
 
 // What a wave has seen of a row.  Lane (kb, n): query head n where tokens or channels are the other index of a product, heads
-// 4 kb + i in the sums.  Weights are p = exp2(x - m + HEADROOM).
-constexpr float HEADROOM = 7.f;      // weights are at most 2^15 (m may lag 2^8 behind the maximum), fp16's normal range reaches down to 2^-21 of m's
-constexpr float LAG = 8.f;
-constexpr float LARGEST = 15.99f;
+// 4 kb + i in the sums.  Weights are p = exp2(x - m), with logits x rounded as m was made of them: logits past 2^24 are so far apart in fp32 that
+// anything taken off before would be rounded otherwise than in the others (from 2^27 on a maximum's own weight was anything from 0 to infinite).
+constexpr float HEADROOM = 7.f;      // m is set this much below the maximum, and may lag behind it until a weight would pass 2^MOST;
+constexpr float MOST = 15.f;         // fp16's normal range reaches down to 2^-21 of a weight that is 2^HEADROOM
 struct Seen {
   float m;                           // of head n, in powers of two
   f32x4 l, acc[8];                   // of head 4 kb + i; channels cb 16 + n
@@ -98,11 +98,11 @@ __device__ __forceinline__ float max_groups(float x) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// The maximum moves up where a weight would otherwise pass the headroom: for most pages it does not.
+// m moves up where a weight would otherwise be too large: for most pages it does not.
 __device__ __forceinline__ void raise(Seen& s, float top, int lane) {
   top = max_groups(top);
-  if (!__any(top > s.m + LAG)) return;
-  const float m = fmaxf(s.m, top), f = exp2f(s.m - m);
+  if (!__any(top - s.m > MOST)) return;
+  const float m = fmaxf(s.m, top - HEADROOM), f = exp2f(s.m - m);
   s.m = m;
   f32x4 g;
 #pragma unroll
@@ -210,19 +210,17 @@ __device__ __forceinline__ float max8(const f32x4* x) {
 }
 
 // Its weights, in fp16, and normalised by the sum of what they were rounded to: half a step of 2^-11 each, 2e-4 of the output on
-// average.  Where the output is fp16 itself, what the rounding left is taken along.  Logits past 2^22 are so far apart in fp32 that a
-// weight may come out at 2^16, which fp16 does not have: it is held to what there is (a NaN stays one).
+// average.  Where the output is fp16 itself, what the rounding left is taken along.
 template <int DT> struct Weights {
   half8 hi, lo;                      // lo: fp16 only
   __device__ __forceinline__ void none() { hi = lo = half8{0, 0, 0, 0, 0, 0, 0, 0}; }
 };
 template <int DT>
 __device__ __forceinline__ Weights<DT> page_weights(const f32x4* x, float f, float b, float m) {
-  const float off = b - (m - HEADROOM);
   Weights<DT> p;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float w = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(fmaf(x[j >> 2][j & 3], f, off), LARGEST));
+    const float w = __builtin_amdgcn_exp2f(fmaf(x[j >> 2][j & 3], f, b) - m);
     p.hi[j] = (_Float16)w;
     if constexpr (DT == 0) p.lo[j] = (_Float16)(w - (float)p.hi[j]);
   }
@@ -283,12 +281,11 @@ __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const 
     }
   raise(s, top, lane);
   // weights in T, and what the rounding left
-  const float off = s.m - HEADROOM;
   uint16_t hi[8], lo[8];
   u32x4 there;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float p = __builtin_amdgcn_exp2f(x[j >> 2][j & 3] - off);
+    const float p = __builtin_amdgcn_exp2f(x[j >> 2][j & 3] - s.m);
     hi[j] = to_T<DT>(p);
     lo[j] = to_T<DT>(p - from_T<DT>(hi[j]));
   }

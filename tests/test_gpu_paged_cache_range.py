@@ -61,3 +61,44 @@ def test_branches_with_wide_queries():
     q[2, ::3, 5] = 2.0 ** 45
     q[4, :, 5] = -2.0 ** 33
     p.check_attention(0, [0, 1, 2, 3, 4], q=q)
+
+
+@pytest.mark.parametrize("keys,queries", [(100, 20), (100, -100), (-100, 100), (-60, -60), (60, 50)])
+def test_logits_of_all_sizes(keys, queries):
+    """Products from far below 1 to near fp32's largest."""
+    p = Pair(n_kv=1, G=3, max_seqs=1, max_ctx=512, n_pages=40)
+    p.grow([0], [300], lambda x, gen: torch.stack((x[0] * 2.0 ** keys, x[1])))
+    p.check_attention(0, [0], scale=2.0 ** queries)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("power", [22, 24, 26, 27, 28, 30])
+def test_tokens_whose_logits_are_the_same_weigh_the_same(power, dtype):
+    """Logits of about 2^power in powers of two, the same at two tokens of three and 0 at the third: the mean of the two's values, whatever
+    the maximum is rounded to when it is set, in full pages, in the open one, and where they are joined.  (Keys are 0 and 15 steps.)"""
+    p = Pair(n_kv=1, G=2, max_seqs=2, max_ctx=4096, n_pages=130, dtype=dtype)
+    key = 15.0 * 2.0 ** 8
+
+    def same(x, gen):
+        x[0] = 0
+        x[0, ..., 0] = key
+        x[0, ::3, :, 0] = 0
+        x[1] = torch.randn(x[1].shape, generator=gen)
+        return x
+
+    p.grow([0, 1], [71, 3011], same)
+    q = torch.zeros((2, 2, D), dtype=TYPES[dtype])
+    size = 2.0 ** power / key * math.sqrt(D) / math.log2(math.e)
+    if dtype == "fp16":
+        size = min(size, 60000.0)
+    q[:, 0, 0], q[:, 1, 0] = size, size * 0.93
+    out = torch.empty_like(q, device="cuda")
+    p.c.attn(0, ints([0, 1]), q.cuda(), out)
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    for s in (0, 1):
+        value, lo, step = p.m.values(0, s)
+        far = p.m.tokens[0][s][:, 0, 0, 0] == 0
+        # the mean's own rounding, that of weights (half a step of 2^-11, which all share), and sums of values of up to 5
+        want = value[~far][:, 1, 0].mean(0)
+        off = (out[s].cpu().double() - want).abs() - half * 1.01 * want.abs() - 2.0 ** -24 * 512 * 5
+        assert float(off.max()) <= 0, s
