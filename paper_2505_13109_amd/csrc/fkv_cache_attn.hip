@@ -27,27 +27,21 @@ __device__ __forceinline__ half8 key_codes(uint32_t w) {
   const u32x4 r = {(w << 4) & nibble, w & nibble, (w >> 4) & nibble, (w >> 8) & nibble};
   return __builtin_bit_cast(half8, r);
 }
-// Values', as VALUE_BASE + code.  The instruction cuts products off some 24 bits below the largest one, and takes a denormal number for
+// Values', as VALUE_BASE + code, in eight.  The instruction cuts products off some 24 bits below the largest one, and takes a denormal number for
 // as large as the smallest normal one.  Logits, whose products have both signs, are off by 1e-5 so; weights, all positive, would lose
-// 2^-15 of their sum on the way, and an output over 128K tokens, small among its values, came out 0.4 % off.
-// 64 + code takes seven instructions and leaves 1e-4 of such an output, for bf16; 16 + code takes eight, for fp16.
+// 2^-15 of their sum on the way, and an output over 128K tokens, small among its values, came out 0.4 % off.  (64 + code takes seven and loses
+// four times what 16 + code does.)
 // (The base's bits come from a register that is not known to be a constant: an instruction takes one constant, and masking and
-// setting are one of three operands so: 32 fewer to a page, which takes some 350.)
-template <int DT> constexpr float VALUE_BASE = DT ? 64.f : 16.f;
-template <int DT> __device__ __forceinline__ uint32_t value_bits() {
-  uint32_t b = DT ? 0x54005400u : 0x4c004c00u;
+// setting are one of three operands so: 32 fewer to a page.)
+constexpr float VALUE_BASE = 16.f;
+__device__ __forceinline__ uint32_t value_bits() {
+  uint32_t b = 0x4c004c00u;
   asm("" : "+v"(b));
   return b;
 }
-template <int DT> __device__ __forceinline__ half8 value_codes(uint32_t w, uint32_t base) {
-  u32x4 r;
-  if constexpr (DT == 1) {
-    constexpr uint32_t nibble = 0x00f000f0u;
-    r = u32x4{((w << 4) & nibble) | base, (w & nibble) | base, ((w >> 4) & nibble) | base, ((w >> 8) & nibble) | base};
-  } else {
-    constexpr uint32_t nibble = 0x03c003c0u;
-    r = u32x4{((w << 6) & nibble) | base, ((w << 2) & nibble) | base, ((w >> 2) & nibble) | base, ((w >> 6) & nibble) | base};
-  }
+__device__ __forceinline__ half8 value_codes(uint32_t w, uint32_t base) {
+  constexpr uint32_t nibble = 0x03c003c0u;
+  const u32x4 r = {((w << 6) & nibble) | base, ((w << 2) & nibble) | base, ((w >> 2) & nibble) | base, ((w >> 6) & nibble) | base};
   return __builtin_bit_cast(half8, r);
 }
 
@@ -209,28 +203,32 @@ __device__ __forceinline__ float max8(const f32x4* x) {
   return top;
 }
 
-// Its weights, in fp16, and normalised by the sum of what they were rounded to: half a step of 2^-11 each, 2e-4 of the output on
-// average.  Where the output is fp16 itself, what the rounding left is taken along.
-template <int DT> struct Weights {
-  half8 hi, lo;                      // lo: fp16 only
+// Its weights, in two fp16 halves, 21 bits: what the upper one leaves behind is taken along in a second product.  With the upper one alone bf16
+// outputs of 32K tokens are 0.6 % further off on average, and one of 30 is another number of bf16; 4 x 128K tokens take 124 us instead of
+// 132, 32K 15.3 instead of 15.8.  (Up to eight heads both could be rows of one product of 16: 129 and 16.0.)
+struct Weights {
+  half8 hi, lo;
   __device__ __forceinline__ void none() { hi = lo = half8{0, 0, 0, 0, 0, 0, 0, 0}; }
 };
-template <int DT>
-__device__ __forceinline__ Weights<DT> page_weights(const f32x4* x, float f, float b, float m) {
-  Weights<DT> p;
+__device__ __forceinline__ Weights page_weights(const f32x4* x, float f, float b, float m) {
+  Weights p;
+  float minus = -1.f;                  // (not known to be that: a product and sum of both types is one instruction, a difference three)
+  asm("" : "+s"(minus));
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float w = __builtin_amdgcn_exp2f(fmaf(x[j >> 2][j & 3], f, b) - m);
-    p.hi[j] = (_Float16)w;
-    if constexpr (DT == 0) p.lo[j] = (_Float16)(w - (float)p.hi[j]);
+  for (int j = 0; j < 8; j += 2) {
+    float w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(x[j >> 2][(j & 3) + i], f, b) - m);
+    const auto hi = __builtin_amdgcn_cvt_pkrtz(w[0], w[1]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      p.hi[j + i] = (_Float16)hi[i];
+      p.lo[j + i] = (_Float16)fmaf((float)hi[i], minus, w[i]);
+    }
   }
   return p;
 }
-template <int DT> __device__ __forceinline__ f32x4 weigh(const Weights<DT>& p, half8 v, f32x4 c) {
-  c = mfma_h(p.hi, v, c);
-  if constexpr (DT == 0) c = mfma_h(p.lo, v, c);
-  return c;
-}
+__device__ __forceinline__ f32x4 weigh(const Weights& p, half8 v, f32x4 c) { return mfma_h(p.lo, v, mfma_h(p.hi, v, c)); }
 
 // Heads g0 to g0 + G - 1, where a page counts for these alone.
 struct Own {
@@ -241,9 +239,9 @@ struct Own {
 // Its values: the weights times the codes, and step and lo of a channel are applied to the page's sums.  ONE: own heads' only (the weights
 // of others are 0, but a NaN among the values would reach them).
 template <int DT, bool ONE>
-__device__ __forceinline__ void page_sums(const Values& r, int info, const Weights<DT>& p, uint32_t bits, Own own, int lane, Seen& s) {
+__device__ __forceinline__ void page_sums(const Values& r, int info, const Weights& p, uint32_t bits, Own own, int lane, Seen& s) {
   const u32x4 ones = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
-  const f32x4 sum = weigh<DT>(p, __builtin_bit_cast(half8, ones), f32x4{0, 0, 0, 0}), base = sum * -VALUE_BASE<DT>;
+  const f32x4 sum = weigh(p, __builtin_bit_cast(half8, ones), f32x4{0, 0, 0, 0}), base = sum * -VALUE_BASE;
   s.l += sum;
   const half8 vstep = __builtin_bit_cast(half8, r.step);
   const float vscale = ldexpf(1.f, exp_of_values(info));
@@ -251,7 +249,7 @@ __device__ __forceinline__ void page_sums(const Values& r, int info, const Weigh
   const uint32_t vw[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) {
-    const f32x4 pv = weigh<DT>(p, value_codes<DT>(vw[cb], bits), base);
+    const f32x4 pv = weigh(p, value_codes(vw[cb], bits), base);
     const float step = (float)vstep[cb] * vscale, lo = (cb & 1) ? Unpack<DT>::hi(lo2[cb >> 1]) : Unpack<DT>::lo(lo2[cb >> 1]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -665,7 +663,7 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
   }
 
   // -- the pages
-  const uint32_t bits = value_bits<DT>();
+  const uint32_t bits = value_bits();
   auto walk = [&](auto one, int first, int end) {
     constexpr bool ONE = decltype(one)::value;
     int g0 = 0;
@@ -696,7 +694,7 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
           return !ONE || own.has(n) ? top : -INFINITY;
         };
         auto weights = [&] {
-          Weights<DT> p = page_weights<DT>(x, f, b, seen.m);
+          Weights p = page_weights(x, f, b, seen.m);
           if (ONE && !own.has(n)) p.none();
           return p;
         };
