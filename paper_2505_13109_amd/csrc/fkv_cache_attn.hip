@@ -79,6 +79,10 @@ __device__ __forceinline__ void load_values(const CacheDesc& c, size_t u, int la
 // anything taken off before would be rounded otherwise than in the others (from 2^27 on a maximum's own weight was anything from 0 to infinite).
 constexpr float HEADROOM = 7.f;      // m is set this much below the maximum, and may lag behind it until a weight would pass 2^MOST;
 constexpr float MOST = 15.f;         // fp16's normal range reaches down to 2^-21 of a weight that is 2^HEADROOM
+// Sums are of weights times 2^DOWN.  bf16 values go up to fp32's largest number, which the sum of weights shall not multiply: 2^22 tokens that weigh
+// the same stay below 1.  (Values of 2^-98 and less are too small for that, over 128K tokens.  A scale chosen by what the sums come to was
+// tried: 12 % more time for 32K tokens.)
+template <int DT> constexpr int DOWN = DT == 1 ? -30 : 0;
 struct Seen {
   float m;                           // of head n, in powers of two
   f32x4 l, acc[8];                   // of head 4 kb + i; channels cb 16 + n
@@ -241,10 +245,12 @@ struct Own {
 template <int DT, bool ONE>
 __device__ __forceinline__ void page_sums(const Values& r, int info, const Weights& p, uint32_t bits, Own own, int lane, Seen& s) {
   const u32x4 ones = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
-  const f32x4 sum = weigh(p, __builtin_bit_cast(half8, ones), f32x4{0, 0, 0, 0}), base = sum * -VALUE_BASE;
+  f32x4 sum = weigh(p, __builtin_bit_cast(half8, ones), f32x4{0, 0, 0, 0});
+  const f32x4 base = sum * -VALUE_BASE;
+  sum *= ldexpf(1.f, DOWN<DT>);
   s.l += sum;
   const half8 vstep = __builtin_bit_cast(half8, r.step);
-  const float vscale = ldexpf(1.f, exp_of_values(info));
+  const float vscale = ldexpf(1.f, exp_of_values(info) + DOWN<DT>);
   const uint32_t lo2[4] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w};
   const uint32_t vw[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
 #pragma unroll
@@ -283,7 +289,7 @@ __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const 
   u32x4 there;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float p = __builtin_amdgcn_exp2f(x[j >> 2][j & 3] - s.m);
+    const float p = __builtin_amdgcn_exp2f(x[j >> 2][j & 3] - s.m) * ldexpf(1.f, DOWN<DT>);
     hi[j] = to_T<DT>(p);
     lo[j] = to_T<DT>(p - from_T<DT>(hi[j]));
   }

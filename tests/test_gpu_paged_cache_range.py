@@ -102,3 +102,40 @@ def test_tokens_whose_logits_are_the_same_weigh_the_same(power, dtype):
         want = value[~far][:, 1, 0].mean(0)
         off = (out[s].cpu().double() - want).abs() - half * 1.01 * want.abs() - 2.0 ** -24 * 512 * 5
         assert float(off.max()) <= 0, s
+
+
+@pytest.mark.parametrize("lens", [[5], [64], [100], [3000, 20, 257]])
+@pytest.mark.parametrize("scale", [0.0, 1.0])
+def test_values_near_the_largest_number(lens, scale):
+    """bf16 values of up to 3e38, in full pages and the open one, alone and joined, among branches; weights all the same or not.  Their mean
+    is a number, and the sums on the way to it have to be."""
+    p = Pair(n_kv=32, G=2, max_seqs=5, max_ctx=4096, n_pages=130)
+    seqs = list(range(len(lens)))
+
+    def large(x, gen):
+        x[1] = torch.sign(x[1]) * 3.0e38 * torch.rand(x[1].shape, generator=gen)
+        x[1, ..., 64:] = x[1, ..., 64:].abs()            # (means near the largest, too)
+        x[1, ..., 100] = 3.3e38                          # (a step of 0)
+        return x
+
+    p.grow(seqs, lens, large)
+    p.check_attention(0, seqs, scale=scale)
+    p.c.fork(ints([0]), ints([4]))
+    p.m.fork([0], [4])
+    p.grow([0, 4], [40, 3], large)
+    p.check_attention(0, seqs + [4], scale=scale)
+
+
+@pytest.mark.parametrize("power", [-100, -60, 60, 110])
+def test_values_of_all_sizes(power):
+    """Outputs as near to the definition as those of values of 1 are, relative to their size."""
+    p = Pair(n_kv=2, G=4, max_seqs=2, max_ctx=512, n_pages=40)
+    p.grow([0, 1], [300, 45], lambda x, gen: torch.stack((x[0], x[1] * 2.0 ** power)))
+    q = p.queries(2)
+    out = torch.empty_like(q, device="cuda")
+    p.c.attn(0, ints([0, 1]), q.cuda(), out)
+    for s in (0, 1):
+        for layer in p.m.tokens:                         # the same of a model whose values are 2^power smaller, where the bound's absolute part counts
+            layer[s] = torch.stack((layer[s][:, 0].double(), layer[s][:, 1].double() * 2.0 ** -power), 1).bfloat16()
+    scaled = (out.double() * 2.0 ** -power).cpu()
+    p.check_attention(0, [0, 1], q=q, got=scaled)
