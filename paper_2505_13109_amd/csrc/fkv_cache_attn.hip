@@ -266,6 +266,12 @@ __device__ __forceinline__ void page_sums(const Values& r, int info, const Weigh
 }
 
 // The open page: `rest` tokens in T.  ONE: own heads'.  Places behind them hold anything, so neither their weights nor their values count.
+// Two numbers of T without those that are not finite.  (The exponent is all ones, to which adding its lowest bit carries into the sign's place.)
+template <int DT> __device__ __forceinline__ uint32_t finite(uint32_t w) {
+  constexpr uint32_t exponent = DT == 0 ? 0x7c00u : 0x7f80u, lowest = exponent & (0u - exponent);
+  const uint32_t carry = ((w & (exponent | exponent << 16)) + (lowest | lowest << 16)) & 0x80008000u;
+  return w & ~((carry >> 15) * 0xffffu);
+}
 template <int DT, bool ONE>
 __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const u32x4* qT, float scale, Own own, int lane, Seen& s) {
   const int kb = lane >> 4, n = lane & 15;
@@ -308,7 +314,9 @@ __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const 
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) {
     const u32x4 v = *reinterpret_cast<const u32x4*>(open + PG * D + ((cb * 4 + kb) * 16 + n) * 8) & there;
-    const f32x4 x = mfma_T<DT>(pl, v, mfma_T<DT>(ph, v, none));
+    // (an infinity times what the rounding left, which is 0 or of any sign, would be NaN)
+    const u32x4 vl = {finite<DT>(v[0]), finite<DT>(v[1]), finite<DT>(v[2]), finite<DT>(v[3])};
+    const f32x4 x = mfma_T<DT>(pl, vl, mfma_T<DT>(ph, v, none));
 #pragma unroll
     for (int i = 0; i < 4; ++i) s.acc[cb][i] += !ONE || own.has(kb * 4 + i) ? x[i] : 0.f;
   }

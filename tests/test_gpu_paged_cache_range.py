@@ -139,3 +139,42 @@ def test_values_of_all_sizes(power):
             layer[s] = torch.stack((layer[s][:, 0].double(), layer[s][:, 1].double() * 2.0 ** -power), 1).bfloat16()
     scaled = (out.double() * 2.0 ** -power).cpu()
     p.check_attention(0, [0, 1], q=q, got=scaled)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("branches", [0, 4])
+def test_an_infinite_value_in_the_open_page_gives_an_infinity(branches, dtype):
+    """Open tokens are kept as they are: a channel with one infinity is infinite, with two of one sign as well, NaN with two signs or a NaN; all
+    others are as if there were none.  Weights that are all of a size."""
+    p = Pair(n_kv=32, G=2, max_seqs=6, max_ctx=1536, n_pages=100, dtype=dtype)
+
+    def bad(x, gen):
+        x[1, 0, 0, 3] = math.inf
+        x[1, 8, 1, 4] = -math.inf
+        x[1, 2, 2, 5], x[1, 9, 2, 5] = math.inf, math.inf
+        x[1, 1, 3, 6], x[1, 3, 3, 6] = math.inf, -math.inf
+        x[1, 5, 4, 7] = math.nan
+        return x
+
+    p.grow([0], [1280])
+    rows = list(range(1 + branches))
+    if branches:
+        p.c.fork(ints([0] * branches), ints(rows[1:]))
+        p.m.fork([0] * branches, rows[1:])
+    s = rows[-1]
+    p.grow([s], [10], bad)
+    for r in rows[:-1]:
+        p.grow([r], [7])
+    q = p.queries(len(rows), 0.1)
+    out = torch.empty_like(q, device="cuda")
+    p.c.attn(0, ints(rows), q.cuda(), out)
+    got = out.cpu()
+    mine = got[-1].view(32, 2, D)
+    assert (mine[0, :, 3] == math.inf).all() and (mine[1, :, 4] == -math.inf).all() and (mine[2, :, 5] == math.inf).all()
+    assert mine[3, :, 6].isnan().all() and mine[4, :, 7].isnan().all()
+    assert int((~torch.isfinite(got)).sum()) == 10
+    for h, channel in ((0, 3), (1, 4), (2, 5), (3, 6), (4, 7)):
+        mine[h, :, channel] = 0
+        p.m.tokens[0][s] = p.m.tokens[0][s].clone()
+        p.m.tokens[0][s][:, 1, h, channel] = 0
+    p.check_attention(0, rows, q=q, got=got)
