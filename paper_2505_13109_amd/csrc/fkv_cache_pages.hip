@@ -30,13 +30,13 @@ __device__ int scan_block(int v, int* total, int* sh) {
   return before + x - v;
 }
 
-// the first entry that names each slot: first[slot], for entries that name one
-__device__ void first_entries(const int32_t* slots, int n, int max_seqs, int* first) {
+// the first entry that names each slot: first[slot], for entries that name one.  Of those whose src is padding none does.
+__device__ void first_entries(const int32_t* slots, const int32_t* src, int n, int max_seqs, int* first) {
   for (int s = threadIdx.x; s < max_seqs; s += (int)blockDim.x) first[s] = n;
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += (int)blockDim.x) {
     const int s = slots[i];
-    if (s >= 0 && s < max_seqs) atomicMin(&first[s], i);
+    if (s >= 0 && s < max_seqs && !(src && src[i] == -1)) atomicMin(&first[s], i);
   }
   __syncthreads();
 }
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_extend_kernel(CacheDesc c,
   int* const base = off + n_rows;                          // where in the tables the row's page 0 would go if it were the pool's 0th
   const int in_use = c.head[CACHE_USED];
   const uint32_t word0 = (int)threadIdx.x < (c.n_pages + 31) / 32 ? c.used[threadIdx.x] : 0u;
-  first_entries(seqs, n_rows, c.max_seqs, first);
+  first_entries(seqs, nullptr, n_rows, c.max_seqs, first);
 
   constexpr int PER = CACHE_MAX_SEQS / PLAN_THREADS;
   const int per = (n_rows + PLAN_THREADS - 1) / PLAN_THREADS;
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_fork_kernel(CacheDesc a, c
   int* const off = first + c.max_seqs;
   const int in_use = COPY ? c.head[CACHE_USED] : 0;
   const uint32_t word0 = COPY && (int)threadIdx.x < (c.n_pages + 31) / 32 ? c.used[threadIdx.x] : 0u;
-  first_entries(dst, n, c.max_seqs, first);
+  first_entries(dst, src, n, c.max_seqs, first);
 
   constexpr int PER = CACHE_MAX_SEQS / PLAN_THREADS;
   const int per = (n + PLAN_THREADS - 1) / PLAN_THREADS;
