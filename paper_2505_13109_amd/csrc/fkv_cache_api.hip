@@ -130,7 +130,7 @@ int check_tokens(fkv_cache* c, int layer, const int32_t* seqs, int n, const int3
   if (n_tokens < 0) return c->fail(FKV_ERANGE, "n_tokens is negative");
   if (!cu && n_tokens != n) return c->fail(FKV_EINVAL, "without token offsets there is one token a row");
   if (!aligned(cu, 4)) return c->fail(FKV_EINVAL, "token offsets: not 4-byte aligned");
-  if (n_tokens == 0) return 1;
+  if (n_tokens == 0) return FKV_OK;
   if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return c->fail(FKV_EINVAL, "keys or values: null or not 16-byte aligned");
   return FKV_OK;
 }
@@ -234,6 +234,7 @@ int fkv_cache_read(fkv_cache* c, int32_t layer, const int32_t* seqs, int32_t n_r
                    void* stream) {
   FKV_CACHE(c);
   FKV_ROWS(check_tokens(c, layer, seqs, n_rows, cu, k, v, n_tokens));
+  if (n_tokens == 0) return FKV_OK;
   launch_cache_read(c->desc, layer, seqs, n_rows, cu, static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), n_tokens, static_cast<hipStream_t>(stream));
   return after_launch(c, "read kernel");
 }

@@ -76,9 +76,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheDesc c, int laye
   const int m = blockIdx.y, tid = threadIdx.x;
   const Piece at_row = piece_of<false>(c, seqs, cu, n_rows, n_tokens, blockIdx.x);
   const int row = at_row.row, piece = at_row.piece, first = at_row.first, n = at_row.n, s = at_row.named, slot = at_row.slot, end = at_row.len;
-  if (piece < 0 || s == -1 || n == 0) return;
+  if (piece < 0 || s == -1) return;
   int32_t* const mark_at = c.appended + ((size_t)layer * c.max_seqs + slot) * c.n_kv + m;
   const int owner = c.owner[slot], added = c.added[slot], serial = c.serial[slot], marked = *mark_at;
+  // A row without tokens is right wherever it has not been given room for some.
+  if (n == 0 && s == slot && (owner != row || added == 0)) return;
   // (the mark is the first piece's own: others go by the unit that they fill)
   if (s != slot || owner != row || added != n || (piece == 0 && marked == serial)) {
     if (piece == 0 && m == 0 && tid == 0) atomicOr(&c.head[CACHE_FAULTS], FAULT_ENTRY);
