@@ -66,7 +66,22 @@ class DecoderStack:
         return torch.cat([a * cos - b * sin, a * sin + b * cos], dim=-1)
 
     def step(self, x, external_qkv=None, stream=None):
-        """x [batch, hidden] -> [batch, hidden].  external_qkv: per layer (q [batch,n_q,d], k, v [batch,n_kv,d])."""
+        """x [batch, hidden] -> [batch, hidden].  external_qkv: per layer (q [batch,n_q,d], k, v [batch,n_kv,d]).
+
+        Over a PagedCache the whole step runs on `stream`, behind what the current stream has been given and before what it is given next:
+        positions come from the device, so the projections have to follow the cache's calls.  Over a FreeKV context, `stream` is the one that
+        its calls are launched on; the rest runs on the current stream, which has to be the same."""
+        here = torch.cuda.current_stream(self.fkv.device) if self.paged and stream is not None else None
+        if here is None or stream == here:
+            return self._step(x, external_qkv, stream)
+        stream.wait_stream(here)
+        with torch.cuda.stream(stream):
+            y = self._step(x, external_qkv, stream)
+        here.wait_stream(stream)
+        y.record_stream(here)
+        return y
+
+    def _step(self, x, external_qkv, stream):
         pos_cached, cos, sin = None, None, None
         if self.paged:
             self.fkv.extend(self.seqs, stream=stream)
