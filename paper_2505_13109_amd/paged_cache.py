@@ -33,6 +33,8 @@ class PagedCache:
         rc = self.L.fkv_cache_arena_bytes(C.byref(self.cfg), C.byref(need))
         if rc:
             raise FreeKVError(f"fkv_cache_arena_bytes: {rc}: {self.L.fkv_cache_last_error(None).decode()}")
+        if self.device.type != "cuda":
+            raise FreeKVError(f"device: a cache is on a GPU, not on {self.device}")
         if not torch.cuda.is_available():
             raise FreeKVError("no GPU: the cache's operators are HIP kernels")
         if self.device.index is None:

@@ -91,8 +91,6 @@ def check_told_apart(p, got, k, v, q, attended=None):
 @pytest.mark.parametrize("kv,G,n", [(1, 6, 130000), (1, 3, 70001), (2, 2, 40010), (1, 1, 20001), (8, 2, 32769), (1, 16, 9000), (4, 3, 2111)])
 def test_every_page_counts_once(kv, G, n, dtype):
     """Up to as many splits as a row may have (256: one KV head and more than 65536 tokens), in one and two levels."""
-    if n > 70001 and dtype == "fp16":
-        pytest.skip("the same cut as in bf16")
     p = Pair(n_kv=kv, G=G, max_seqs=1, max_ctx=-(-n // PG) * PG, n_pages=n // PG + 1, dtype=dtype)
     k, v = told_apart(p, 0, n)
     q = group_queries(p)
