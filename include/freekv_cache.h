@@ -90,14 +90,18 @@ int fkv_cache_append(fkv_cache* cache, int32_t layer, const int32_t* seqs_dev, i
 /* o_h = softmax(q_h K^T / sqrt(d)) V over what the cache holds of row i's sequence, one query token a row:
  * q, out dev [n_rows, n_q, d] of T, 16-byte aligned.  Several rows may name one sequence.
  *   pages_dev  NULL: every token.  Otherwise dev [n_rows, n_kv, n_list] i32, per KV head the positions (page 0 holds tokens
- *              0 to 31) of the full pages to attend, as fkv_page_select emits them, next to the first sink_tokens and the
+ *              0 to 31) of the full pages to attend, in the form of fkv_page_select's lists, next to the first sink_tokens and the
  *              last window_tokens tokens' full pages (both multiples of page_size, the sink first if they overlap) and the
  *              open page, which are attended always.  Entries that are not a full page between sink and window
  *              (-1, say) are passed over; one that is listed twice counts twice.  n_list: 0 to 131072.
- * Branches among up to 64 rows of a call with G <= 8 read the pages that they shared at their last fork together, whatever the
- * rows' order.
- * Softmax and sums are in fp32, the output is rounded once.  A row that has nothing to attend (padding, an empty sequence,
- * an empty list) gets zeros. */
+ * Branches read pages that they shared at their last fork together, 16 / G rows at most at a time, whatever the rows' order, in
+ * calls without lists of 2 to 64 rows with G <= 8, where they share 8 pages or more and the rows have more than 4096 / n_kv pages in
+ * all.  The cache must have been forked by then: a graph that was captured before its first fork reads each row's pages for itself, as does
+ * every other call.  The result is the same up to rounding.
+ * Logits, softmax and sums are in fp32, the output is rounded once.  bf16 outputs of less than 2^-98 lose digits; values of any size
+ * do not overflow up to 2^22 tokens that weigh about the same.  A row that has nothing to attend (padding, an empty sequence,
+ * an empty list), or whose logits are all minus infinity, gets zeros.  An infinite value in the open page gives an infinity, NaN where
+ * its token weighs less than 2^-30 of the largest. */
 int fkv_cache_attn(fkv_cache* cache, int32_t layer, const int32_t* seqs_dev, int32_t n_rows, const void* q_dev,
                    const int32_t* pages_dev, int32_t n_list, int32_t sink_tokens, int32_t window_tokens, void* out_dev,
                    void* stream);
@@ -108,7 +112,7 @@ int fkv_cache_read(fkv_cache* cache, int32_t layer, const int32_t* seqs_dev, int
                    void* k_dev, void* v_dev, int32_t n_tokens, void* stream);
 
 /* Sequence dst[i] becomes what src[i] is, for i < n: it shares src's full pages and gets a copy of its open page.  dst[i] must be
- * empty when the call begins; a slot may be the source of many. */
+ * empty when the call begins; a slot may be the source of many.  An entry whose source or target is -1 is padding. */
 int fkv_cache_fork(fkv_cache* cache, const int32_t* src_dev, const int32_t* dst_dev, int32_t n, void* stream);
 
 /* The same with pages of its own: sequence src[i] of `from` is copied to the empty slot dst[i] of `to`, into the lowest free

@@ -118,7 +118,7 @@ __device__ __forceinline__ void raise(Seen& s, float top, int lane) {
 // far below, where a query's large channels meet keys that hardly change in them.  A logit loses up to 128 channels x code 15 x 3 x 2^-25 (a
 // rounding of q16 times a step of up to 2, and one of the low half), 2^(E + q_exp - 29) with the powers of two and 1 / sqrt(128): 2^-17 where they
 // add up to WIDE.  Beyond, the halves are of each page's products relative to the largest of them: 128K x 4 tokens take
-// 213 us where all pages are such instead of 122.
+// 223 us where all pages are such instead of 132.
 constexpr int WIDE = 12;
 
 // Eight channels in fp32, not known to the compiler to be the same for every page: it would keep all of them in registers.
@@ -208,8 +208,8 @@ __device__ __forceinline__ float max8(const f32x4* x) {
 }
 
 // Its weights, in two fp16 halves, 21 bits: what the upper one leaves behind is taken along in a second product.  With the upper one alone bf16
-// outputs of 32K tokens are 0.6 % further off on average, and one of 30 is another number of bf16; 4 x 128K tokens take 124 us instead of
-// 132, 32K 15.3 instead of 15.8.  (Up to eight heads both could be rows of one product of 16: 129 and 16.0.)
+// outputs of 32K tokens are 0.6 % further off on average, and one of 30 is another number of bf16; 4 x 128K tokens take 125 us instead of
+// 133, 32K 15.4 instead of 15.9.  (Up to eight heads both could be rows of one product of 16: 130 and 16.2.)
 struct Weights {
   half8 hi, lo;
   __device__ __forceinline__ void none() { hi = lo = half8{0, 0, 0, 0, 0, 0, 0, 0}; }
@@ -322,11 +322,11 @@ __device__ __forceinline__ void open_page(const uint16_t* open, int rest, const 
   }
 }
 
-// 256 blocks of eight waves take as long (32K tokens, 32/8 heads, 15.4 us either way, 128K x 4 126 against 124) but leave ragged
-// batches less to balance with (36 against 28); three waves to a SIMD, 168 registers and 768 blocks, 19.2, 142 and 34.
+// 256 blocks of eight waves take as long (32K tokens, 32/8 heads, 16.1 us against 15.9, 128K x 4 136 against 133) but leave ragged
+// batches less to balance with (39 against 29); three waves to a SIMD, 168 registers and 768 blocks, 19.6, 144 and 34.
 constexpr int WAVES = 4, THREADS = WAVES * 64;
-// Splits that are joined at once, and how many there may be for one level of that.  By 16: 32K tokens 16.4 us, lists of 4096 tokens for
-// eight requests 18.6 against 16.0.
+// Splits that are joined at once, and how many there may be for one level of that.  By 16: 32K tokens 16.9 us, lists of 4096 tokens for
+// eight requests 18.3 against 16.3.
 constexpr int JOIN = 8, ONE_LEVEL = 12;
 
 // How a row's attention is cut: positions are the pages to attend in order (sink, list, window, or all), the open page last.
@@ -374,7 +374,7 @@ __device__ __forceinline__ int scan_wave(int v) {
 //
 // There is room for CACHE_ATTN_BLOCKS blocks at once, so for `room` splits of all rows together.  Rows are cut into equal chunks: of a
 // few sizes, from the one that lengths without remainders would allow to the one that any lengths do, the smallest that leaves no
-// split for a second round (32 requests of 500 to 16K tokens, 28/4 heads: 28 us; with about as many splits as there is room
+// split for a second round (32 requests of 500 to 16K tokens, 28/4 heads: 29 us; with about as many splits as there is room
 // 34).  Where there are more rows than half the room, about as many splits as there is room.
 struct Place {
   int row, split, n_splits;
@@ -420,7 +420,7 @@ __device__ __forceinline__ Place place_of(int item, int n_rows, int n_kv, int la
 
 // Rows that are branches of one sequence.  A page's products have 16 columns and a row has G heads, so up to 16 / G rows are taken
 // together: as one row of that many times the heads, whose positions are the pages that they share and then each one's own, which count for
-// its heads only.  32 branches of 16 sequences of up to 8K tokens, 32/8 heads: 32 us a layer instead of 43.  A fork leaves with its
+// its heads only.  32 branches of 16 sequences of up to 8K tokens, 32/8 heads: 33 us a layer instead of 46.  A fork leaves with its
 // branches how many pages they share (`kin`).  The last of these pages names them: a page has one place in all the tables that have it,
 // and the same ones before it.  Where splits are as small as they get anyhow, time is not in the pages and rows stay by themselves.
 // positions: of all that are taken together for the first, -1 for the others.
@@ -454,7 +454,7 @@ __device__ __forceinline__ Kin kin_of(const CacheDesc& c, Cut& cut, int n_rows, 
 }
 
 // Values that blocks of one launch hand each other: at device scope, past the caches of one XCD.  A fence would write back all that
-// its L2 holds (28 us of 52 for 32K tokens, 70 of 202 for four times 128K); these stores are in memory when they count as done.
+// its L2 holds (28 us of the 52 that 32K tokens took with fences, 70 of 202 for four times 128K); these stores are in memory when they count as done.
 __device__ __forceinline__ void hand_on(unsigned long long* p, float a, float b) {
   __hip_atomic_store(p, (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -819,7 +819,7 @@ __global__ __launch_bounds__(THREADS, 2) void attn_cache_kernel(CacheDesc c, Cac
 
 void launch_cache_attn(const CacheDesc& c, const CacheAttn& a, bool forked, hipStream_t st) {
   const int grid = cache_attn_items(a.n_rows, c.n_kv) * c.n_kv;
-  // (32 ragged rows that are no branches take 27.9 us instead of 27.1 where they are looked for)
+  // (32 ragged rows that are no branches take 29.8 us instead of 29.2 where they are looked for)
   const bool kin = forked && !a.pages && a.n_rows > 1 && a.n_rows <= CACHE_KIN_ROWS && 2 * c.G <= CACHE_MAX_G;
   auto launch = [&](auto kernel) { kernel<<<grid, THREADS, 0, st>>>(c, a); };
   if (c.dtype == 0) kin ? launch(attn_cache_kernel<0, true>) : launch(attn_cache_kernel<0, false>);
