@@ -12,3 +12,4 @@ from .binding import (  # noqa: F401
     FkvConfig, FreeKV, FreeKVError, lib, lib_path, EXPORTED_SYMBOLS,
 )
 from .paged_cache import PagedCache  # noqa: F401
+from .projection import empty_quant, proj_gate, proj_matmul, proj_norm, proj_quant, proj_rope  # noqa: F401

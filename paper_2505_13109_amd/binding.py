@@ -1,4 +1,4 @@
-"""ctypes binding of include/freekv.h and include/freekv_cache.h.  Argument marshalling only."""
+"""ctypes binding of include/freekv.h, include/freekv_cache.h and include/freekv_proj.h.  Argument marshalling only."""
 from __future__ import annotations
 
 import ctypes as C
@@ -28,6 +28,7 @@ EXPORTED_SYMBOLS = (
     "fkv_cache_arena_bytes", "fkv_cache_create", "fkv_cache_destroy", "fkv_cache_last_error", "fkv_cache_health", "fkv_cache_used_pages",
     "fkv_cache_extend", "fkv_cache_append", "fkv_cache_attn", "fkv_cache_read", "fkv_cache_fork", "fkv_cache_copy", "fkv_cache_free",
     "fkv_cache_compact", "fkv_cache_tables",
+    "fkv_proj_last_error", "fkv_proj_quant", "fkv_proj_norm", "fkv_proj_gate", "fkv_proj_rope", "fkv_proj_matmul", "fkv_proj_workspace",
 )
 
 
@@ -125,6 +126,13 @@ def lib() -> C.CDLL:
         "fkv_cache_free": (C.c_int, [vp, vp, i32, vp]),
         "fkv_cache_compact": (C.c_int, [vp, vp]),
         "fkv_cache_tables": (C.c_int, [vp, vp, i32, vp, vp, vp]),
+        "fkv_proj_last_error": (C.c_char_p, []),
+        "fkv_proj_quant": (C.c_int, [i32, i32, vp, i32, i32, i32, vp, vp, vp]),
+        "fkv_proj_norm": (C.c_int, [i32, i32, vp, vp, vp, i32, i32, C.c_float, vp, vp, vp, vp, vp]),
+        "fkv_proj_gate": (C.c_int, [i32, i32, vp, i32, i32, vp, vp, vp]),
+        "fkv_proj_rope": (C.c_int, [i32, i32, vp, i32, i32, i32, vp, i32, C.POINTER(i32), vp, vp, vp, vp, vp]),
+        "fkv_proj_matmul": (C.c_int, [i32, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]),
+        "fkv_proj_workspace": (C.c_int, [i32, i32, i32, C.POINTER(sz)]),
     })
     for name, (res, args) in sig.items():
         fn = getattr(L, name)

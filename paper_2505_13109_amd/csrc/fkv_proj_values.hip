@@ -1,0 +1,249 @@
+// Values into 8 bits: as they are, behind the norm, behind the gated activation.  Bound by memory: every value is read once.
+// A thread has eight adjacent columns (16 bytes of T), so a block of 128 is a row of 16 lanes and its largest value four steps away.
+#include "fkv_proj_dev.h"
+
+#include <type_traits>
+
+namespace fkv {
+
+namespace {
+
+constexpr int CHUNK = 8;
+
+__device__ __forceinline__ uint4 load16(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
+
+// ---- plain values, and the gate: a thread one chunk of a row -------------------------------------------------
+
+// g / (1 + exp(-g)) u.  exp(-|g|) = 2^hi (1 + lo ln 2) with hi + lo = -|g| log2(e) to 48 bits; the product g u is exact for bf16, 22 of
+// 24 bits for fp16, so that what is left is about one rounding of the sigmoid and one of the result.
+__device__ __forceinline__ float gated(float g, float u) {
+  const float a = -fabsf(g);
+  const float hi = a * 0x1.715476p+0f, lo = fmaf(a, 0x1.4ae0c0p-26f, fmaf(a, 0x1.715476p+0f, -hi));
+  const float p = __builtin_amdgcn_exp2f(hi);
+  const float t = fmaf(p, lo * 0x1.62e430p-1f, p);
+  const float d = 1.f + t, y = __builtin_amdgcn_rcpf(d);
+  const float n = g < 0.f ? t : 1.f;
+  // n / d from the reciprocal: the remainder counts what d was rounded by, too
+  const float s = n * y, rem = fmaf(-s, d, n) - s * (t - (d - 1.f));
+  return g * u * fmaf(rem, y, s);
+}
+
+template <int DT, bool GATE>
+__global__ __launch_bounds__(256) void proj_quant_kernel(const uint16_t* x, int64_t n_chunks, int row_chunks, int cols, uint8_t* codes, float* scales) {
+  // row_chunks: chunks of a row, up to the end of its last block
+  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = c / row_chunks;
+  const int at = (int)(c - row * row_chunks) * CHUNK;
+  const bool in = c < n_chunks && at < cols;
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  if (in) {
+    if (GATE) {
+      const uint16_t* p = x + row * 2 * cols + at;
+      const uint4 gw = load16(p), uw = load16(p + cols);
+      float g[8], u[8];
+      unpack8<DT>(gw, g);
+      unpack8<DT>(uw, u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = gated(g[i], u[i]);
+    } else {
+      unpack8<DT>(load16(x + row * cols + at), v);
+    }
+  }
+  const Quant q = quant_of(top_of_16(top_bits(v)));
+  if (in) {
+    *reinterpret_cast<uint2*>(codes + row * cols + at) = codes_of(q, v);
+    if (at % QB == 0) scales[row * (row_chunks * CHUNK / QB) + at / QB] = scale_of(q);
+  }
+}
+
+// 128 rows a scale: a block of 256 threads has one of weights, in registers
+template <int DT>
+__global__ __launch_bounds__(256) void proj_quant_tile_kernel(const uint16_t* x, int rows, int cols, int blocks, uint8_t* codes, float* scales) {
+  __shared__ uint32_t s_top[4];
+  const int64_t r0 = (int64_t)(blockIdx.x / blocks) * QB;
+  const int b = blockIdx.x % blocks, at = b * QB + (threadIdx.x & 15) * CHUNK;
+  uint4 w[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = r0 + (threadIdx.x >> 4) + 16 * i;
+    w[i] = row < rows && at < cols ? load16(x + row * cols + at) : make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float v[8];
+    unpack8<DT>(w[i], v);
+    const uint32_t t = top_bits(v);
+    top = t > top ? t : top;
+  }
+  top = wave_reduce_u32(top, OpMaxU32());
+  if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = s_top[0];
+#pragma unroll
+  for (int i = 1; i < 4; ++i) top = s_top[i] > top ? s_top[i] : top;
+  const Quant q = quant_of(top);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = r0 + (threadIdx.x >> 4) + 16 * i;
+    if (row < rows && at < cols) {
+      float v[8];
+      unpack8<DT>(w[i], v);
+      *reinterpret_cast<uint2*>(codes + row * cols + at) = codes_of(q, v);
+    }
+  }
+  if (threadIdx.x == 0) scales[r0 / QB * blocks + b] = scale_of(q);
+}
+
+// ---- the norm: a block a row -----------------------------------------------------------------------------------
+
+// Codes are those of s weight, which the inputs alone decide; the row's factor goes into the scales.  So a chunk's codes are written
+// before the row's sum is known, and only a scale waits for it.  Squares are summed in fp64: they pass fp32's range where bf16 values do
+// not.  CH chunks a thread are in registers (of a row that is longer, so many at a time: its products are made again for `out`).
+template <int DT, int NT, int CH, bool ADD, bool OUT>
+__global__ __launch_bounds__(NT) void proj_norm_kernel(ProjNorm a) {
+  __shared__ double s_sum[NT / 64];
+  const int64_t row = blockIdx.x;
+  const int blocks = blocks_of(a.cols), first = threadIdx.x * CHUNK;
+  const uint16_t* x = a.x + row * a.cols;
+  const uint16_t* add = a.add + (ADD ? row * a.cols : 0);
+  uint16_t* res = a.res + (a.res ? row * a.cols : 0);
+  uint8_t* codes = a.codes + (a.codes ? row * a.cols : 0);
+  float* scales = a.scales + (a.codes ? row * blocks : 0);
+  float z[CH][8], scale[CH];
+  auto load = [&](int at, uint4* w) {          // x, add, weight
+    w[0] = load16(x + at);
+    if (ADD) w[1] = load16(add + at);
+    if (a.weight) w[2] = load16(a.weight + at);
+  };
+  auto sum_of = [&](const uint4* w, float* v) {
+    unpack8<DT>(w[0], v);
+    if (ADD) {
+      float t[8];
+      unpack8<DT>(w[1], t);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += t[i];
+      unpack8<DT>(pack8<DT>(v), v);
+    }
+  };
+  auto times_weight = [&](const uint4& w, float* v) {
+    if (!a.weight) return;
+    float t[8];
+    unpack8<DT>(w, t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= t[i];
+  };
+  double sum = 0.0;
+  for (int base = 0; base < blocks * QB; base += NT * CHUNK * CH) {
+    uint4 w[CH][3];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const int at = base + j * NT * CHUNK + first;
+      w[j][0] = w[j][1] = w[j][2] = make_uint4(0, 0, 0, 0);
+      if (at < a.cols) load(at, w[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const int at = base + j * NT * CHUNK + first;
+      const bool in = at < a.cols;
+      sum_of(w[j], z[j]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fma((double)z[j][i], (double)z[j][i], sum);
+      if (ADD && a.res && in) *reinterpret_cast<uint4*>(res + at) = pack8<DT>(z[j]);
+      times_weight(w[j][2], z[j]);
+      if (a.codes) {
+        const Quant q = quant_of(top_of_16(top_bits(z[j])));
+        scale[j] = scale_of(q);
+        if (in) {
+          *reinterpret_cast<uint2*>(codes + at) = codes_of(q, z[j]);
+          if (base + NT * CHUNK * CH < blocks * QB && at % QB == 0) scales[at / QB] = scale[j];
+        }
+      }
+    }
+  }
+  sum = wave_sum_f64(sum);
+  if ((threadIdx.x & 63) == 63) s_sum[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < NT / 64; ++i) sum += s_sum[i];
+  const double m = sum / (double)a.cols + (double)a.eps;
+  // the instruction's 2^-26 and a step of Newton's; an infinite value in the row leaves 0
+  double r = __builtin_amdgcn_rsq(m);
+  r = m < __builtin_inf() ? r * fma(-0.5 * m * r, r, 1.5) : m == m ? 0.0 : m;
+  const int last = (blocks * QB - 1) / (NT * CHUNK * CH) * (NT * CHUNK * CH);
+  for (int base = 0; base < blocks * QB; base += NT * CHUNK * CH) {
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const int at = base + j * NT * CHUNK + first;
+      if (at >= a.cols) continue;
+      if (a.codes && at % QB == 0) {
+        const float s = base == last ? scale[j] : scales[at / QB];
+        scales[at / QB] = (float)((double)s * r);
+      }
+      if (OUT) {
+        float v[8];
+        if (base == last) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = z[j][i];
+        } else {
+          uint4 w[3];
+          load(at, w);
+          if (ADD && a.res) unpack8<DT>(load16(res + at), v);
+          else sum_of(w, v);
+          times_weight(w[2], v);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)((double)v[i] * r);
+        *reinterpret_cast<uint4*>(a.out + row * a.cols + at) = pack8<DT>(v);
+      }
+    }
+  }
+}
+
+template <typename F>
+void by_type(int dtype, F f) {
+  if (dtype == 0) f(std::integral_constant<int, 0>());
+  else f(std::integral_constant<int, 1>());
+}
+template <typename F>
+void by_flag(bool flag, F f) {
+  if (flag) f(std::true_type());
+  else f(std::false_type());
+}
+
+}  // namespace
+
+void launch_proj_quant(int dtype, const uint16_t* x, int rows, int cols, int tile, uint8_t* codes, float* scales, hipStream_t st) {
+  const int blocks = blocks_of(cols);
+  by_type(dtype, [&](auto dt) {
+    if (tile == 1) {
+      const int64_t n = (int64_t)rows * blocks * (QB / CHUNK);
+      hipLaunchKernelGGL((proj_quant_kernel<dt(), false>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, st, x, n, blocks * (QB / CHUNK), cols, codes, scales);
+    } else {
+      hipLaunchKernelGGL((proj_quant_tile_kernel<dt()>), dim3((uint32_t)blocks * blocks_of(rows)), dim3(256), 0, st, x, rows, cols, blocks, codes, scales);
+    }
+  });
+}
+
+void launch_proj_gate(int dtype, const uint16_t* gu, int rows, int cols, uint8_t* codes, float* scales, hipStream_t st) {
+  const int blocks = blocks_of(cols);
+  const int64_t n = (int64_t)rows * blocks * (QB / CHUNK);
+  by_type(dtype, [&](auto dt) {
+    hipLaunchKernelGGL((proj_quant_kernel<dt(), true>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, st, gu, n, blocks * (QB / CHUNK), cols, codes, scales);
+  });
+}
+
+void launch_proj_norm(int dtype, const ProjNorm& a, hipStream_t st) {
+  by_type(dtype, [&](auto dt) {
+    by_flag(a.add != nullptr, [&](auto add) {
+      by_flag(a.out != nullptr, [&](auto out) {
+        hipLaunchKernelGGL((proj_norm_kernel<dt(), 512, 2, add(), out()>), dim3((uint32_t)a.rows), dim3(512), 0, st, a);
+      });
+    });
+  });
+}
+
+}  // namespace fkv
