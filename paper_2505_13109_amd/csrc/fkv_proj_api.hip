@@ -43,7 +43,14 @@ int check(int dtype, int rows, int cols) {
   if (dtype != FKV_DTYPE_FP16 && dtype != FKV_DTYPE_BF16) return fail(FKV_EINVAL, "dtype must be fp16 or bf16");
   if (rows < 0 || rows > PROJ_MAX_ROWS) return fail(FKV_ERANGE, "rows must be 0 to 4194304");
   if (cols < 16 || cols > PROJ_MAX_COLS || cols % 16) return fail(FKV_ERANGE, "cols must be a multiple of 16 up to 131072");
+  // (a launch has fewer than 2^32 threads)
+  if ((int64_t)rows * blocks_of(cols) >= 1 << 28) return fail(FKV_ERANGE, "rows x ceil(cols / 128) must be below 268435456");
   return rows == 0;
+}
+int check_n(int rows, int n) {
+  if (n < 1 || n > PROJ_MAX_ROWS) return fail(FKV_ERANGE, "n must be 1 to 4194304");
+  if ((int64_t)rows * n > (int64_t)1 << 37) return fail(FKV_ERANGE, "rows x n must be at most 2^37");
+  return FKV_OK;
 }
 
 template <typename Launch>
@@ -113,16 +120,16 @@ int fkv_proj_rope(int32_t device, int32_t dtype, const void* qkv, int32_t rows, 
 
 int fkv_proj_workspace(int32_t rows, int32_t n, int32_t cols, size_t* bytes) {
   if (!bytes) return fail(FKV_EINVAL, "null");
-  if (n < 1 || n > PROJ_MAX_ROWS) return fail(FKV_ERANGE, "n must be 1 to 4194304");
   const int rc = check(FKV_DTYPE_BF16, rows, cols);
   if (rc < 0) return rc;
+  if (const int bad = check_n(rows, n)) return bad;
   *bytes = rc ? 0 : proj_matmul_work(rows, n, cols);
   return FKV_OK;
 }
 
 int fkv_proj_matmul(int32_t device, int32_t dtype, const void* x, const float* xs, const void* w, const float* ws, int32_t rows, int32_t n, int32_t cols,
                     void* out, void* work, size_t work_bytes, void* stream) {
-  if (n < 1 || n > PROJ_MAX_ROWS) return fail(FKV_ERANGE, "n must be 1 to 4194304");
+  FKV_PROJ(check_n(rows, n));
   FKV_PROJ(check(dtype, rows, cols));
   if (!fits(x) || !fits(xs) || !fits(w) || !fits(ws) || !fits(out)) return fail(FKV_EINVAL, "codes, scales or out: null or not 16-byte aligned");
   const size_t need = proj_matmul_work(rows, n, cols);

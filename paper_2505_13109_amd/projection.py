@@ -8,6 +8,7 @@ is done with them; `stream` None is the current stream of the tensors' device.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 
 import torch
@@ -15,6 +16,7 @@ import torch
 from .binding import FreeKVError, lib
 
 BLOCK = 128
+FEW_ROWS = 64                 # up to here a product needs no workspace
 CODES = torch.float8_e4m3fn
 _TYPES = {torch.float16: 0, torch.bfloat16: 1}
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
@@ -141,5 +143,11 @@ def proj_matmul(codes, scales, w, w_scales, out, stream=None):
     blocks = -(-cols // BLOCK)
     x, xs = _at(codes, "codes", CODES, (rows, cols), dev), _at(scales, "scales", torch.float32, (rows, blocks), dev)
     ww, ws = _at(w, "w", CODES, (n, cols), dev), _at(w_scales, "w_scales", torch.float32, (-(-n // BLOCK), blocks), dev)
-    L = lib()
-    _run(L.fkv_proj_matmul, "fkv_proj_matmul", dev, t, x, xs, ww, ws, rows, n, cols, at, None, 0, stream=stream)
+    work, size = None, 0
+    if rows > FEW_ROWS:
+        need = C.c_size_t()
+        if lib().fkv_proj_workspace(rows, n, cols, C.byref(need)) == 0 and need.value:
+            size = need.value
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):     # (the stream's own memory: it is free again behind this call's work)
+                work = torch.empty(size, dtype=torch.uint8, device=out.device)
+    _run(lib().fkv_proj_matmul, "fkv_proj_matmul", dev, t, x, xs, ww, ws, rows, n, cols, at, None if work is None else work.data_ptr(), size, stream=stream)

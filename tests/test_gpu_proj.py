@@ -321,6 +321,9 @@ def product(x, xs, w, ws, dtype):
     return out
 
 
+FEW = 64               # rows up to which no product is cut
+
+
 # 128 products a block and the blocks' sums, each addition off by a step of fp32 of the terms' sizes at most, and the scales' product and its own
 def sum_off(cols):
     return (128 + -(-cols // 128) + 3) * 2.0 ** -23
@@ -336,7 +339,7 @@ WIDTHS = [(1, 16), (15, 112), (16, 128), (17, 144), (128, 1024), (129, 2064), (3
 def test_product_is_the_definition(rows, n, cols, dtype):
     x, xs, w, ws = operands(rows, n, cols, seed=rows + n)
     want, size, cut = M.matmul(x, xs, w, ws)
-    near(product(x, xs, w, ws, dtype), want, half_step(dtype) * 1.01, sum_off(cols) * size + cut + 2.0 ** -25)
+    near(product(x, xs, w, ws, dtype), want, half_step(dtype) * 1.01, sum_off(cols) * size + (rows > FEW) * cut + 2.0 ** -25)
 
 
 @pytest.mark.parametrize("rows,n,cols", [(1, 300, 4096), (7, 4096, 11056), (40, 1031, 2048), (130, 513, 1040), (300, 700, 8192), (1030, 1100, 1024)])
@@ -362,7 +365,7 @@ def test_product_keeps_rows_columns_and_blocks_apart(rows):
     x, xs, w, ws = operands(rows, n, cols, seed=9)
     xs = xs * torch.exp2(torch.randint(-30, 30, xs.shape, generator=gen(1)).float())
     clean, size, cut = M.matmul(x, xs, w, ws)
-    near(product(x, xs, w, ws, torch.bfloat16), clean, half_step(torch.bfloat16) * 1.01, sum_off(cols) * size + cut)
+    near(product(x, xs, w, ws, torch.bfloat16), clean, half_step(torch.bfloat16) * 1.01, sum_off(cols) * size + (rows > FEW) * cut)
     xs[rows // 2, 3] = math.nan
     ws[1, 8] = math.nan
     wf = w.float()
@@ -374,7 +377,7 @@ def test_product_keeps_rows_columns_and_blocks_apart(rows):
     bad[:, 128:256] = True
     bad[:, 399] = True
     assert torch.equal(torch.isnan(got), bad)
-    off = half_step(torch.bfloat16) * 1.01 * clean.abs() + sum_off(cols) * size + cut
+    off = half_step(torch.bfloat16) * 1.01 * clean.abs() + sum_off(cols) * size + (rows > FEW) * cut
     assert ((got.double() - clean).abs()[~bad] <= off[~bad]).all()
 
 
