@@ -172,7 +172,10 @@ template <int DT, int TN, int TM, int WN, int WM, bool SPLIT>
 __global__ __launch_bounds__(WN * WM * 64) void proj_many_kernel(ProjMatmul a, Tiles g) {
   constexpr int NW = WN * WM, AN = TN / WN / 16, AM = TM / WM / 16, ROWS = TN + TM, LOADS = ROWS / 8 / NW;
   static_assert(ROWS % (8 * NW) == 0 && TN % (8 * NW) == 0 && TN / WN <= QB && QB % (TN / WN) == 0, "");
+  constexpr int SB = 8, WB = (TN + QB - 1) / QB;
+  static_assert(TM * SB == 4 * NW * 64 && SB * WB <= NW * 64, "");
   __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2][ROWS * QB];
+  __shared__ float s_xs[2][SB][TM], s_ws[2][SB][WB];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, gr = lane >> 4;
   // tiles dealt to the XCDs in runs; within a run eight tiles of rows, then the next of columns
   const int total = g.tn * g.tm * g.splits;
@@ -201,55 +204,84 @@ __global__ __launch_bounds__(WN * WM * 64) void proj_many_kernel(ProjMatmul a, T
     load_lds(is_w ? wbuf : xbuf, off, lds + stage * (ROWS * QB) + r * QB);
   };
   const int wn = wave % WN, wm = wave / WN;
-  const float* wsp = a.ws + (int64_t)((c0 + wn * (TN / WN)) / QB < blocks_of(a.n) ? (c0 + wn * (TN / WN)) / QB : 0) * blocks;
-  const float* sp[AM];
+  // Scales of SB blocks at a time: a row's lie behind each other in memory and are wanted row by row, so they go through LDS, too.
+  auto scales_from = [&](int b, float* v) {
+    const int r = threadIdx.x / (SB / 4);
+    const float* from = a.xs + min(r0 + r, (int64_t)a.rows - 1) * blocks;
 #pragma unroll
-  for (int j = 0; j < AM; ++j) sp[j] = a.xs + min(r0 + wm * (TM / WM) + 16 * j + t, (int64_t)a.rows - 1) * blocks;
+    for (int k = 0; k < 4; ++k) v[k] = from[min(b + (int)(threadIdx.x % (SB / 4)) * 4 + k, blocks - 1)];
+    const int wb = min(c0 / QB + (int)threadIdx.x / SB, blocks_of(a.n) - 1);
+    v[4] = a.ws[(int64_t)(threadIdx.x < SB * WB ? wb : 0) * blocks + min(b + (int)threadIdx.x % SB, blocks - 1)];
+  };
+  auto scales_to = [&](int which, const float* v) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s_xs[which][threadIdx.x % (SB / 4) * 4 + k][threadIdx.x / (SB / 4)] = v[k];
+    if (threadIdx.x < SB * WB) s_ws[which][threadIdx.x % SB][threadIdx.x / SB] = v[4];
+  };
   float4v acc[AN][AM];
 #pragma unroll
   for (int i = 0; i < AN; ++i)
 #pragma unroll
     for (int j = 0; j < AM; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
-  float xs[AM], ws = 0.f;
+  float s[AM], s_before[AM], scales[5];
+  scales_from(b0, scales);
+  float4v p[2][AM];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) bring(b0, 0, i);
 #pragma unroll
-  for (int j = 0; j < AM; ++j) xs[j] = sp[j][b0];
-  ws = wsp[b0];
+  for (int j = 0; j < AM; ++j) {
+    s_before[j] = 0.f;
+    p[1][j] = float4v{0.f, 0.f, 0.f, 0.f};
+  }
+  scales_to(0, scales);
   const int lo = t * QB + ((gr ^ (t & 7)) * 16), hi = lo ^ 64;
+  static_assert(AN % 2 == 0, "");
   for (int b = b0; b < b1; ++b) {
     const int stage = (b - b0) & 1;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    float s[AM];
+    const uint8_t* base = &s_tile[stage][0];
+    auto operand = [&](int row) {
+      const uint4 q = *reinterpret_cast<const uint4*>(base + row * QB + lo), r = *reinterpret_cast<const uint4*>(base + row * QB + hi);
+      return word8{(int)q.x, (int)q.y, (int)q.z, (int)q.w, (int)r.x, (int)r.y, (int)r.z, (int)r.w};
+    };
+    // Products of a step go into sums a step later, so that neither waits for the other; operands are asked for two steps ahead.
+    word8 xv[AM], wv[3];
+    wv[0] = operand(wn * (TN / WN));
 #pragma unroll
-    for (int j = 0; j < AM; ++j) s[j] = xs[j] * ws;
+    for (int j = 0; j < AM; ++j) xv[j] = operand(TN + wm * (TM / WM) + 16 * j);
+    wv[1] = operand(wn * (TN / WN) + 16);
+    const int nth = b - b0, which = nth / SB & 1;
+    const float ws = s_ws[which][nth % SB][wn * (TN / WN) / QB];
+#pragma unroll
+    for (int j = 0; j < AM; ++j) s[j] = s_xs[which][nth % SB][wm * (TM / WM) + 16 * j + t] * ws;
     if (b + 1 < b1) {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) bring(b + 1, stage ^ 1, i);
-#pragma unroll
-      for (int j = 0; j < AM; ++j) xs[j] = sp[j][b + 1];
-      ws = wsp[b + 1];
     }
-    const uint8_t* base = &s_tile[stage][0];
-    auto operand = [&](int row) {
-      const uint4 p = *reinterpret_cast<const uint4*>(base + row * QB + lo), q = *reinterpret_cast<const uint4*>(base + row * QB + hi);
-      return word8{(int)p.x, (int)p.y, (int)p.z, (int)p.w, (int)q.x, (int)q.y, (int)q.z, (int)q.w};
-    };
-    word8 xv[AM];
-#pragma unroll
-    for (int j = 0; j < AM; ++j) xv[j] = operand(TN + wm * (TM / WM) + 16 * j);
+    if (nth % SB == 0) scales_from(b + SB, scales);
+    if (nth % SB == SB / 2) scales_to(which ^ 1, scales);
 #pragma unroll
     for (int i = 0; i < AN; ++i) {
-      const word8 wv = operand(wn * (TN / WN) + 16 * i);
+      if (i + 2 < AN) wv[(i + 2) % 3] = operand(wn * (TN / WN) + 16 * (i + 2));
 #pragma unroll
       for (int j = 0; j < AM; ++j) {
-        const float4v p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv[j], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        p[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[i % 3], xv[j], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+        const float f = i ? s[j] : s_before[j];
+        float4v& c = acc[i ? i - 1 : AN - 1][j];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[j], p[e], acc[i][j][e]);
+        for (int e = 0; e < 4; ++e) c[e] = fmaf(f, p[(i + 1) & 1][j][e], c[e]);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
+#pragma unroll
+    for (int j = 0; j < AM; ++j) s_before[j] = s[j];
   }
+#pragma unroll
+  for (int j = 0; j < AM; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[AN - 1][j][e] = fmaf(s_before[j], p[1][j][e], acc[AN - 1][j][e]);
 #pragma unroll
   for (int j = 0; j < AM; ++j) {
     const int64_t row = r0 + wm * (TM / WM) + 16 * j + t;
