@@ -6,6 +6,7 @@
 // scale of activations) and four adjacent columns.
 #include "fkv_proj_dev.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace fkv {
@@ -33,14 +34,38 @@ __device__ __forceinline__ void store4(uint16_t* out, int64_t row, int c, int n,
   if (c + 3 < n) p[3] = (uint16_t)(b >> 16);
 }
 
+// ---- codes into LDS ------------------------------------------------------------------------------------------------
+
+// 16 bytes of each lane into LDS behind each other, from `at` on; zeros where an offset is past the buffer's end
+__device__ __forceinline__ void load_lds(const int4v& buffer, uint32_t offset, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
+}
+// the same of 4 bytes
+__device__ __forceinline__ void load_lds4(const int4v& buffer, uint32_t offset, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
+__device__ __forceinline__ int4v buffer_of(const uint8_t* p, uint32_t bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  int4v r = {(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)bytes, 0x00020000};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
+  return r;
+}
+// The same value, which the compiler takes for a new one: what is worked out from it is not kept in registers through the loop before.
+__device__ __forceinline__ uint32_t anew(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+constexpr uint32_t PAST = 0x80000000u;      // beyond any tile's bytes, also with a row's offset on top
+
 // ---- few rows: bound by the weights' bytes --------------------------------------------------------------------------
-// A block has 16 NT columns and all rows; its waves take the blocks of 128 in turn and their sums meet in LDS.  A wave loads weights and
-// activations straight into operands: lane l has 16 bytes at 16 (l / 16) and at 64 + 16 (l / 16) of row l % 16, so a load takes 64 bytes of each row
-// (which columns an operand's bytes are does not matter as long as both operands have the same).
+// A block has 16 NT columns and all rows; its waves take the blocks of 128 in turn, each by itself, and their sums meet in LDS at the end.
+// Codes go straight into LDS, whole lines of memory at a time, PD blocks of each wave ahead: what is on its way takes no registers, and a wave waits
+// for nobody else.  16 bytes at place p of a row there are those at p ^ (row % 8) of the 128, so that the lanes of a wave, which want the same
+// columns of 16 rows, find them in different banks.
 // Codes are turned into fp16, exactly: the fp16 instruction adds in fp32, where the 8-bit one cuts off what is below 2^-13 of the largest
 // product of eight, and memory leaves the time for it.
-
-__device__ const uint4 g_zeros[2] = {};
 
 __device__ __forceinline__ void halves_of(const uint4& w, half8v* h) {       // 16 codes
   const uint32_t v[4] = {w.x, w.y, w.z, w.w};
@@ -54,90 +79,98 @@ __device__ __forceinline__ void halves_of(const uint4& w, half8v* h) {       // 
   }
 }
 
-template <int MT, int NT>
-struct FewStage {
-  uint4 w[NT][2], x[MT][2];
-  float xs[MT], ws;
-};
+constexpr int FEW_RUN = 128;                 // blocks of 128 whose scales are in LDS at a time
 
-template <int DT, int MT, int NT, int NW>
+template <int DT, int MT, int NT, int NW, int PD>
 __global__ __launch_bounds__(NW * 64) void proj_few_kernel(ProjMatmul a) {
-  __shared__ float4v s_acc[NW][MT * NT][64];
+  constexpr int STAGE = (NT + MT) * 16 * QB, LOADS = (NT + MT) * 2, RING = NW * PD * STAGE, SUMS = NW * MT * NT * 64 * 16;
+  __shared__ __attribute__((aligned(1024))) uint8_t s_ring[RING > SUMS ? RING : SUMS];
+  __shared__ float s_xs[(16 * MT * (FEW_RUN + 1) + 63) / 64 * 64], s_ws[FEW_RUN];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
   const int blocks = blocks_of(a.cols), c0 = blockIdx.x * 16 * NT;
-  const uint8_t *wp[NT], *xp[MT];
-  const float *sp[MT], *wsp = a.ws + (int64_t)(c0 / QB) * blocks;
+  const int4v wbuf = buffer_of(a.w + (int64_t)c0 * a.cols, (uint32_t)min(16 * NT, a.n - c0) * (uint32_t)a.cols), xbuf = buffer_of(a.x, (uint32_t)a.rows * (uint32_t)a.cols);
+  const int4v wsbuf = buffer_of((const uint8_t*)(a.ws + (int64_t)(c0 / QB) * blocks), (uint32_t)blocks * 4), xsbuf = buffer_of((const uint8_t*)a.xs, (uint32_t)(a.rows * blocks) * 4);
+  const uint32_t ring = lds_of(s_ring) + wave * (PD * STAGE), chunk = ((lane & 7) ^ (lane >> 3)) * 16, from = (uint32_t)(lane >> 3) * (uint32_t)a.cols + chunk;
+  auto bring = [&](int b, int slot) {
+    const uint32_t off = b * QB + (int)chunk < a.cols ? from + (uint32_t)(b * QB) : PAST;
 #pragma unroll
-  for (int j = 0; j < NT; ++j) wp[j] = a.w + (int64_t)min(c0 + 16 * j + t, a.n - 1) * a.cols;       // (what is beyond the ends is not written)
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int row = min(16 * i + t, a.rows - 1);
-    xp[i] = a.x + (int64_t)row * a.cols;
-    sp[i] = a.xs + (int64_t)row * blocks;
-  }
-  auto load = [&](int b, FewStage<MT, NT>& f) {
-    const int lo = b * QB + 16 * g, hi = lo + 64;
-    const bool in_lo = lo < a.cols, in_hi = hi < a.cols;
-    // behind the last column: weights of the row's beginning, times zeros
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      f.w[j][0] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const word4*>(wp[j] + (in_lo ? lo : 0))));
-      f.w[j][1] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const word4*>(wp[j] + (in_hi ? hi : 0))));
+    for (int i = 0; i < LOADS; ++i) {
+      const bool is_w = i < 2 * NT;
+      load_lds(is_w ? wbuf : xbuf, off + (uint32_t)(i - (is_w ? 0 : 2 * NT)) * 8 * (uint32_t)a.cols, ring + slot * STAGE + i * 1024);
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      f.x[i][0] = *(in_lo ? reinterpret_cast<const uint4*>(xp[i] + lo) : g_zeros);
-      f.x[i][1] = *(in_hi ? reinterpret_cast<const uint4*>(xp[i] + hi) : g_zeros);
-      f.xs[i] = sp[i][b];
-    }
-    f.ws = wsp[b];
   };
   float4v acc[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
-  auto take = [&](const FewStage<MT, NT>& f) {
-    half8v w[NT][4];
+  const int lo = t * QB + ((g ^ (t & 7)) * 16), hi = lo ^ 64;
+  for (int run = 0; run < blocks; run += FEW_RUN) {
+    const int end = min(blocks, run + FEW_RUN), held = end - run, pitch = held | 1;        // (rows of scales begin in different banks)
+    if (run) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");               // everybody is done with the scales before
+    for (int e = wave * 64; e < a.rows * pitch; e += NW * 64) {
+      const int i = e + lane, r = i / pitch, b = i - r * pitch;
+      load_lds4(xsbuf, r < a.rows && b < held ? (uint32_t)(r * blocks + run + b) * 4u : PAST, lds_of(s_xs) + e * 4);
+    }
+    for (int e = wave * 64; e < held; e += NW * 64) load_lds4(wsbuf, (uint32_t)(run + e + lane) * 4u, lds_of(s_ws) + e * 4);
+    int b = run + wave, asked = b;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) halves_of(f.w[j][0], w[j]), halves_of(f.w[j][1], w[j] + 2);
+    for (int i = 0; i < PD; ++i)
+      if (asked < end) bring(asked, i), asked += NW;
+    // loads end in order: the scales are there when no more than the stages' are on their way
+    if (b + (PD - 1) * NW < end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PD * LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_barrier" ::: "memory");
+    for (int slot = 0; b < end; b += NW, slot = slot + 1 < PD ? slot + 1 : 0) {
+      if (b + (PD - 1) * NW < end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((PD - 1) * LOADS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const uint8_t* stage = s_ring + wave * (PD * STAGE) + slot * STAGE;
+      uint4 w[NT][2], x[MT][2];
+      float s[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      half8v x[4];
-      halves_of(f.x[i][0], x), halves_of(f.x[i][1], x + 2);
-      const float s = f.xs[i] * f.ws;
+      for (int j = 0; j < NT; ++j) w[j][0] = *reinterpret_cast<const uint4*>(stage + j * 16 * QB + lo), w[j][1] = *reinterpret_cast<const uint4*>(stage + j * 16 * QB + hi);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        float4v p = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < MT; ++i) x[i][0] = *reinterpret_cast<const uint4*>(stage + (NT + i) * 16 * QB + lo), x[i][1] = *reinterpret_cast<const uint4*>(stage + (NT + i) * 16 * QB + hi);
+      const float ws = s_ws[b - run];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[j][k], x[k], p, 0, 0, 0);
+      for (int i = 0; i < MT; ++i) s[i] = s_xs[(16 * i + t) * pitch + b - run] * ws;
+      if (asked < end) {
+        // the operands are in registers, so their place is free
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        bring(asked, slot);
+        asked += NW;
+      }
+      half8v wh[NT][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s, p[e], acc[i][j][e]);
+      for (int j = 0; j < NT; ++j) halves_of(w[j][0], wh[j]), halves_of(w[j][1], wh[j] + 2);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        half8v xh[4];
+        halves_of(x[i][0], xh), halves_of(x[i][1], xh + 2);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          float4v p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[j][k], xh[k], p, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[i], p[e], acc[i][j][e]);
+        }
       }
     }
-  };
-  if (wave < blocks) {
-    FewStage<MT, NT> f[2];
-    load(wave, f[0]);
-    for (int b = wave; b < blocks; b += 2 * NW) {
-      load(min(b + NW, blocks - 1), f[1]);
-      take(f[0]);
-      if (b + NW >= blocks) break;
-      load(min(b + 2 * NW, blocks - 1), f[0]);
-      take(f[1]);
-    }
   }
+  __syncthreads();
+  float4v* sums = reinterpret_cast<float4v*>(s_ring);              // [wave][tile][lane]
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) s_acc[wave][i * NT + j][lane] = acc[i][j];
+    for (int j = 0; j < NT; ++j) sums[(wave * MT * NT + i * NT + j) * 64 + lane] = acc[i][j];
   __syncthreads();
   for (int e = threadIdx.x; e < MT * NT * 64; e += NW * 64) {
     const int tile = e >> 6, l = e & 63, row = 16 * (tile / NT) + (l & 15);
-    float4v v = s_acc[0][tile][l];
+    float4v v = sums[e];
 #pragma unroll
     for (int i = 1; i < NW; ++i) {
-      const float4v u = s_acc[i][tile][l];
+      const float4v u = sums[i * MT * NT * 64 + e];
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] += u[k];
     }
@@ -147,156 +180,273 @@ __global__ __launch_bounds__(NW * 64) void proj_few_kernel(ProjMatmul a) {
 }
 
 // ---- many rows: tiles through LDS ---------------------------------------------------------------------------------------
-// A block has TN columns and TM rows, its waves WN x WM parts of that.  The codes of a block of 128 columns go straight into LDS, while those
-// of the one before are multiplied; 16 bytes at place p of a row there are those at p ^ (row % 8) of the 128, so that the lanes of a wave, which
-// want the same columns of 16 rows, find them in different banks.
-
-// 16 bytes of each lane into LDS behind each other, from `at` on; zeros where an offset is past the buffer's end
-__device__ __forceinline__ void load_lds(const int4v& buffer, uint32_t offset, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
-}
-__device__ __forceinline__ int4v buffer_of(const uint8_t* p, uint32_t bytes) {
-  const uint64_t at = reinterpret_cast<uint64_t>(p);
-  int4v r = {(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)bytes, 0x00020000};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
-  return r;
-}
+// A block works on tiles of TN columns and TM rows, one behind the other, its waves on WN x WM parts of them.  The codes of a block of 128 columns
+// go straight into LDS, ST - 1 of them ahead of the one that is multiplied (of the next tile, where this one's have been asked for), so that
+// neither the operands nor the results of a tile are waited for; 16 bytes at place p of a row there are those at p ^ (row % 8) of the 128, so
+// that the lanes of a wave, which want the same columns of 16 rows, find them in different banks.
 
 struct Tiles {
   int tn, tm;                 // columns' and rows' tiles
   int splits, per;            // parts of the blocks of 128, blocks of a part
 };
-
-template <int DT, int TN, int TM, int WN, int WM, bool SPLIT>
-__global__ __launch_bounds__(WN * WM * 64) void proj_many_kernel(ProjMatmul a, Tiles g) {
-  constexpr int NW = WN * WM, AN = TN / WN / 16, AM = TM / WM / 16, ROWS = TN + TM, LOADS = ROWS / 8 / NW;
-  static_assert(ROWS % (8 * NW) == 0 && TN % (8 * NW) == 0 && TN / WN <= QB && QB % (TN / WN) == 0, "");
-  constexpr int SB = 8, WB = (TN + QB - 1) / QB;
-  static_assert(TM * SB == 4 * NW * 64 && SB * WB <= NW * 64, "");
-  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2][ROWS * QB];
-  __shared__ float s_xs[2][SB][TM], s_ws[2][SB][WB];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, gr = lane >> 4;
-  // tiles dealt to the XCDs in runs; within a run eight tiles of rows, then the next of columns
-  const int total = g.tn * g.tm * g.splits;
-  int id = blockIdx.x;
-  {
-    const int each = total / 8, more = total % 8, x = id % 8, i = id / 8;
-    id = x * each + min(x, more) + i;
-  }
-  const int split = id / (g.tn * g.tm);
-  id -= split * (g.tn * g.tm);
+struct Tile {
+  int split, c0, b0, b1;
+  int64_t r0;
+};
+// Tiles dealt to the XCDs in runs (blocks go to them in turn); within a run eight tiles of rows, then the next of columns.
+template <int TN, int TM>
+__device__ __forceinline__ Tile tile_of(const Tiles& g, int blocks, int id) {
+  const int total = g.tn * g.tm * g.splits, each = total / 8, more = total % 8, x = id % 8;
+  id = x * each + min(x, more) + id / 8;
+  Tile t;
+  t.split = id / (g.tn * g.tm);
+  id -= t.split * (g.tn * g.tm);
   const int group = 8 * g.tn, first = id / group * 8, high = min(8, g.tm - first);
-  const int tm = first + (id % group) % high, tn = (id % group) / high;
-  const int64_t r0 = (int64_t)tm * TM;
-  const int c0 = tn * TN, blocks = blocks_of(a.cols);
-  const int b0 = split * g.per, b1 = min(blocks, b0 + g.per);
-  // what a lane brings: LOADS times 16 bytes, of rows of the weights first
-  const int4v wbuf = buffer_of(a.w + (int64_t)c0 * a.cols, (uint32_t)min(TN, a.n - c0) * (uint32_t)a.cols);
-  const int4v xbuf = buffer_of(a.x + r0 * a.cols, (uint32_t)min((int64_t)TM, a.rows - r0) * (uint32_t)a.cols);
-  const int lrow = lane >> 3, chunk = ((lane & 7) ^ lrow) * 16;
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&s_tile[0][0];
-  auto bring = [&](int b, int stage, int i) {
-    const int r = (i * NW + wave) * 8;
-    const bool is_w = i * NW * 8 < TN;
-    const int at = b * QB + chunk;
-    const uint32_t off = at < a.cols ? (uint32_t)(r - (is_w ? 0 : TN) + lrow) * (uint32_t)a.cols + (uint32_t)at : 0xfffffff0u;
-    load_lds(is_w ? wbuf : xbuf, off, lds + stage * (ROWS * QB) + r * QB);
+  t.r0 = (int64_t)(first + (id % group) % high) * TM;
+  t.c0 = (id % group) / high * TN;
+  t.b0 = t.split * g.per;
+  t.b1 = min(blocks, t.b0 + g.per);
+  return t;
+}
+
+// SB: blocks of 128 whose scales go through LDS at a time
+template <int DT, int TN, int TM, int WN, int WM, int ST, int SB, bool SPLIT>
+__global__ __launch_bounds__(WN * WM * 64) void proj_many_kernel(ProjMatmul a, Tiles g) {
+  constexpr int NW = WN * WM, CN = TN / WN, CM = TM / WM, AN = CN / 16, AM = CM / 16, ROWS = TN + TM, LOADS = ROWS / 8 / NW;
+  constexpr int WB = (TN + QB - 1) / QB, SE = TM * SB / (NW * 64);             // blocks of weights, scales a thread
+  constexpr int OC = CN < 64 ? CN : 64, OS = OC / 8;                           // columns of results on their way out, and 16-byte parts of a row
+  constexpr bool EARLY = ST == 2;                                              // a stage is filled again before its products are done
+  static_assert(ROWS % (8 * NW) == 0 && TN % (8 * NW) == 0 && CN <= QB && QB % CN == 0 && AN % 2 == 0 && ST >= 2 && (!EARLY || AN >= 4), "");
+  static_assert(SE >= 1 && SE <= SB && SE * NW * 64 == TM * SB && SB * WB <= NW * 64, "");
+  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[ST][ROWS * QB];
+  __shared__ float s_xs[2][SB][TM], s_ws[2][SB][WB];
+  __shared__ __attribute__((aligned(16))) uint16_t s_out[SPLIT ? 1 : NW][16 * OC];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, gr = lane >> 4;
+  const int wn = wave % WN, wm = wave / WN, total = g.tn * g.tm * g.splits, blocks = blocks_of(a.cols);
+
+  // The stream of blocks that are brought, ahead of those that are multiplied; zeros behind its end, into stages that nobody reads.
+  Tile here = tile_of<TN, TM>(g, blocks, blockIdx.x);
+  int4v wbuf, xbuf;
+  int lid = blockIdx.x, lb = here.b0, lb_end = here.b1, slot = ST - 1;
+  uint32_t off = PAST;
+  auto buffers = [&](const Tile& to) {
+    wbuf = buffer_of(a.w + (int64_t)to.c0 * a.cols, (uint32_t)min(TN, a.n - to.c0) * (uint32_t)a.cols);
+    xbuf = buffer_of(a.x + to.r0 * a.cols, (uint32_t)min((int64_t)TM, a.rows - to.r0) * (uint32_t)a.cols);
   };
-  const int wn = wave % WN, wm = wave / WN;
-  // Scales of SB blocks at a time: a row's lie behind each other in memory and are wanted row by row, so they go through LDS, too.
-  auto scales_from = [&](int b, float* v) {
-    const int r = threadIdx.x / (SB / 4);
-    const float* from = a.xs + min(r0 + r, (int64_t)a.rows - 1) * blocks;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = from[min(b + (int)(threadIdx.x % (SB / 4)) * 4 + k, blocks - 1)];
-    const int wb = min(c0 / QB + (int)threadIdx.x / SB, blocks_of(a.n) - 1);
-    v[4] = a.ws[(int64_t)(threadIdx.x < SB * WB ? wb : 0) * blocks + min(b + (int)threadIdx.x % SB, blocks - 1)];
-  };
-  auto scales_to = [&](int which, const float* v) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s_xs[which][threadIdx.x % (SB / 4) * 4 + k][threadIdx.x / (SB / 4)] = v[k];
-    if (threadIdx.x < SB * WB) s_ws[which][threadIdx.x % SB][threadIdx.x / SB] = v[4];
-  };
-  float4v acc[AN][AM];
-#pragma unroll
-  for (int i = 0; i < AN; ++i)
-#pragma unroll
-    for (int j = 0; j < AM; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
-  float s[AM], s_before[AM], scales[5];
-  scales_from(b0, scales);
-  float4v p[2][AM];
-#pragma unroll
-  for (int i = 0; i < LOADS; ++i) bring(b0, 0, i);
-#pragma unroll
-  for (int j = 0; j < AM; ++j) {
-    s_before[j] = 0.f;
-    p[1][j] = float4v{0.f, 0.f, 0.f, 0.f};
-  }
-  scales_to(0, scales);
-  const int lo = t * QB + ((gr ^ (t & 7)) * 16), hi = lo ^ 64;
-  static_assert(AN % 2 == 0, "");
-  for (int b = b0; b < b1; ++b) {
-    const int stage = (b - b0) & 1;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const uint8_t* base = &s_tile[stage][0];
-    auto operand = [&](int row) {
-      const uint4 q = *reinterpret_cast<const uint4*>(base + row * QB + lo), r = *reinterpret_cast<const uint4*>(base + row * QB + hi);
-      return word8{(int)q.x, (int)q.y, (int)q.z, (int)q.w, (int)r.x, (int)r.y, (int)r.z, (int)r.w};
-    };
-    // Products of a step go into sums a step later, so that neither waits for the other; operands are asked for two steps ahead.
-    word8 xv[AM], wv[3];
-    wv[0] = operand(wn * (TN / WN));
-#pragma unroll
-    for (int j = 0; j < AM; ++j) xv[j] = operand(TN + wm * (TM / WM) + 16 * j);
-    wv[1] = operand(wn * (TN / WN) + 16);
-    const int nth = b - b0, which = nth / SB & 1;
-    const float ws = s_ws[which][nth % SB][wn * (TN / WN) / QB];
-#pragma unroll
-    for (int j = 0; j < AM; ++j) s[j] = s_xs[which][nth % SB][wm * (TM / WM) + 16 * j + t] * ws;
-    if (b + 1 < b1) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) bring(b + 1, stage ^ 1, i);
+  buffers(here);
+  auto begin = [&]() {
+    if (lb == lb_end && lid < total) {
+      lid += gridDim.x;
+      if (lid < total) {
+        const Tile to = tile_of<TN, TM>(g, blocks, lid);
+        buffers(to);
+        lb = to.b0;
+        lb_end = to.b1;
+      }
     }
-    if (nth % SB == 0) scales_from(b + SB, scales);
-    if (nth % SB == SB / 2) scales_to(which ^ 1, scales);
+    const uint32_t l = anew(lane), chunk = ((l & 7) ^ (l >> 3)) * 16;
+    off = lid < total && lb * QB + (int)chunk < a.cols ? (wave * 8 + (l >> 3)) * (uint32_t)a.cols + chunk + (uint32_t)(lb * QB) : PAST;
+    lb += lid < total;
+    slot = slot + 1 < ST ? slot + 1 : 0;
+  };
+  auto bring = [&](int i) {
+    const int r = i * NW * 8;
+    const bool is_w = r < TN;
+    load_lds(is_w ? wbuf : xbuf, off + (uint32_t)(r - (is_w ? 0 : TN)) * (uint32_t)a.cols, lds_of(s_tile) + slot * (ROWS * QB) + (r + wave * 8) * QB);
+  };
+  // Scales of SB blocks at a time: a row's lie behind each other in memory and are wanted row by row.
+  float scales[SE + 1];
+  int sid = blockIdx.x, sb = here.b0, sb_end = here.b1, sc0 = here.c0;
+  int64_t sr0 = here.r0;
+  auto scales_from = [&]() {
+    if (sb >= sb_end) {
+      sid += gridDim.x;
+      if (sid >= total) return;
+      const Tile to = tile_of<TN, TM>(g, blocks, sid);
+      sb = to.b0, sb_end = to.b1, sc0 = to.c0, sr0 = to.r0;
+    }
+    const uint32_t tid = wave * 64 + anew(lane);
+    const int e = tid % (SB / SE) * SE, r = min((int64_t)(tid / (SB / SE)), a.rows - 1 - sr0);
+    const float* p = a.xs + sr0 * blocks;
 #pragma unroll
-    for (int i = 0; i < AN; ++i) {
-      if (i + 2 < AN) wv[(i + 2) % 3] = operand(wn * (TN / WN) + 16 * (i + 2));
+    for (int k = 0; k < SE; ++k) scales[k] = p[(uint32_t)(r * blocks + min(sb + e + k, blocks - 1))];
+    const int wb = min(tid < SB * WB ? (int)tid / SB : 0, blocks_of(a.n) - 1 - sc0 / QB);
+    scales[SE] = (a.ws + (int64_t)(sc0 / QB) * blocks)[(uint32_t)(wb * blocks + min(sb + (int)tid % SB, blocks - 1))];
+    sb += SB;
+  };
+  auto scales_to = [&](int which) {
+    const uint32_t tid = wave * 64 + anew(lane);
+#pragma unroll
+    for (int k = 0; k < SE; ++k) s_xs[which][tid % (SB / SE) * SE + k][tid / (SB / SE)] = scales[k];
+    if (tid < SB * WB) s_ws[which][tid % SB][tid / SB] = scales[SE];
+  };
+
+  const int lo = t * QB + ((gr ^ (t & 7)) * 16), hi = lo ^ 64;
+  auto operand = [&](int stage, int row) {
+    const uint8_t* base = &s_tile[0][0] + stage * (ROWS * QB) + row * QB;
+    const uint4 q = *reinterpret_cast<const uint4*>(base + lo), r = *reinterpret_cast<const uint4*>(base + hi);
+    return word8{(int)q.x, (int)q.y, (int)q.z, (int)q.w, (int)r.x, (int)r.y, (int)r.z, (int)r.w};
+  };
+  auto row_w = [&](int i) { return wn * CN + 16 * i; };
+  auto row_x = [&](int j) { return TN + wm * CM + 16 * j; };
+
+  // Loads are asked for one at a time between the products: a wave that asks for many at once waits for room in the queue.
+  // With two stages there is one meeting a block, before the last two steps.  By then every wave has this block's operands and what it asked for
+  // of the next, so the rest of the products cover the first operands of the next block, and the next but one is asked for: LOADS / 2 now, the
+  // others in the first steps of the next block.
+  constexpr int NA = LOADS / 2;
+  scales_from();
+#pragma unroll
+  for (int st = 0; st < ST - 1; ++st) {
+    begin();
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) bring(i);
+  }
+  scales_to(0);
+  word8 xv[AM], wv[4];
+  if (EARLY) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    begin();
+#pragma unroll
+    for (int i = 0; i < NA; ++i) bring(i);
+    wv[0] = operand(0, row_w(0));
+    wv[1] = operand(0, row_w(1));
+#pragma unroll
+    for (int j = 0; j < AM; ++j) xv[j] = operand(0, row_x(j));
+  }
+  int stage = 0, which = 0;
+  for (int id = blockIdx.x; id < total; id += gridDim.x) {
+    float4v acc[AN][AM], p[AM];
+    float s[AM], s_before[AM];
+#pragma unroll
+    for (int j = 0; j < AM; ++j) {
+#pragma unroll
+      for (int i = 0; i < AN; ++i) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
+      s_before[j] = 0.f;
+      p[j] = float4v{0.f, 0.f, 0.f, 0.f};
+    }
+    // The product of step i into p, and what was there, of step i - 1 (of the block before), into its sum: neither waits for the other.
+    auto multiply = [&](int i, int j) {
+      const float f = i ? s[j] : s_before[j];
+      float4v& c = acc[i ? i - 1 : AN - 1][j];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[e] = fmaf(f, p[j][e], c[e]);
+      asm volatile("" : "+v"(c));            // (here, and not where the sum is wanted)
+      p[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[i % 4], xv[j], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int nth = 0;
+    for (int b = here.b0; b < here.b1; ++b) {
+      const bool last = nth == SB - 1 || b + 1 == here.b1;
+      if (!EARLY) {
+        // loads end in order: what was asked for behind this stage may still be on its way
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((ST - 2) * LOADS) : "memory");
+        wv[0] = operand(stage, row_w(0));
+#pragma unroll
+        for (int j = 0; j < AM; ++j) xv[j] = operand(stage, row_x(j));
+        wv[1] = operand(stage, row_w(1));
+      }
+      const float ws = s_ws[which][nth][wn * CN / QB];
+#pragma unroll
+      for (int j = 0; j < AM; ++j) s[j] = s_xs[which][nth][wm * CM + 16 * j + t] * ws;
+      if (!EARLY && last && nth) scales_to(which ^ 1);
+      if (nth == 0) scales_from();
+      if (!EARLY && last && !nth) scales_to(which ^ 1);
+      if (!EARLY) begin();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < (EARLY ? AN - 2 : AN); ++i) {
+        if (i + 2 < AN) wv[(i + 2) % 4] = operand(stage, row_w(i + 2));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < AM; ++j) {
+          multiply(i, j);
+          // (its place among the loads: of the first two steps, or of all)
+          constexpr int PLACES = EARLY ? 2 * AM : AN * AM, N = EARLY ? LOADS - NA : LOADS;
+          const int at = i * AM + j;
+          if (at < PLACES)
+#pragma unroll
+            for (int k = at * N / PLACES; k < (at + 1) * N / PLACES; ++k) bring(EARLY ? NA + k : k);
+        }
+      }
+      stage = stage + 1 < ST ? stage + 1 : 0;
+      if (EARLY) {
+        if (last) scales_to(which ^ 1);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        begin();
+        wv[0] = operand(stage, row_w(0));
+        wv[1] = operand(stage, row_w(1));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j <= AM; ++j) {
+          if (j < AM) multiply(AN - 2, j);
+          if (j) {
+            multiply(AN - 1, j - 1);
+            xv[j - 1] = operand(stage, row_x(j - 1));
+          }
+          if (j < AM)
+#pragma unroll
+            for (int k = j * NA / AM; k < (j + 1) * NA / AM; ++k) bring(k);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < AM; ++j) s_before[j] = s[j];
+      nth = last ? 0 : nth + 1;
+      which ^= last;
+    }
+#pragma unroll
+    for (int j = 0; j < AM; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[AN - 1][j][e] = fmaf(s_before[j], p[j][e], acc[AN - 1][j][e]);
+
+    const int cw = here.c0 + wn * CN, out_lane = (int)anew(lane), out_t = out_lane & 15, out_gr = out_lane >> 4;
+    if (SPLIT) {
 #pragma unroll
       for (int j = 0; j < AM; ++j) {
-        __builtin_amdgcn_sched_barrier(0);
-        p[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[i % 3], xv[j], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-        const float f = i ? s[j] : s_before[j];
-        float4v& c = acc[i ? i - 1 : AN - 1][j];
+        const int64_t row = here.r0 + wm * CM + 16 * j + out_t;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = fmaf(f, p[(i + 1) & 1][j][e], c[e]);
+        for (int i = 0; i < AN; ++i) {
+          const int c = cw + 16 * i + 4 * out_gr;
+          if (row < a.rows && c < a.n) *reinterpret_cast<float4v*>(a.work + ((int64_t)here.split * a.rows + row) * ((a.n + 3) / 4 * 4) + c) = acc[i][j];
+        }
       }
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    } else if (a.n % 8) {
 #pragma unroll
-    for (int j = 0; j < AM; ++j) s_before[j] = s[j];
-  }
+      for (int j = 0; j < AM; ++j) {
+        const int64_t row = here.r0 + wm * CM + 16 * j + out_t;
 #pragma unroll
-  for (int j = 0; j < AM; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[AN - 1][j][e] = fmaf(s_before[j], p[1][j][e], acc[AN - 1][j][e]);
-#pragma unroll
-  for (int j = 0; j < AM; ++j) {
-    const int64_t row = r0 + wm * (TM / WM) + 16 * j + t;
-    if (row >= a.rows) continue;
-#pragma unroll
-    for (int i = 0; i < AN; ++i) {
-      const int c = c0 + wn * (TN / WN) + 16 * i + 4 * gr;
-      const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-      if (SPLIT) {
-        if (c < a.n) *reinterpret_cast<float4v*>(a.work + ((int64_t)split * a.rows + row) * ((a.n + 3) / 4 * 4) + c) = acc[i][j];
-      } else {
-        store4<DT>(a.out, row, c, a.n, v);
+        for (int i = 0; i < AN; ++i) {
+          const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+          if (row < a.rows) store4<DT>(a.out, row, cw + 16 * i + 4 * out_gr, a.n, v);
+        }
       }
+    } else {
+      // through LDS, a wave by itself: 16 rows of OC columns, whole lines of the result
+      uint16_t* tile = s_out[wave];
+#pragma unroll
+      for (int j = 0; j < AM; ++j)
+#pragma unroll
+        for (int o = 0; o < CN; o += OC) {
+#pragma unroll
+          for (int i = 0; i < OC / 16; ++i) {
+            const float4v& v = acc[o / 16 + i][j];
+            *reinterpret_cast<uint2*>(tile + out_t * OC + ((2 * i + (out_gr >> 1)) ^ (out_t & (OS - 1))) * 8 + (out_gr & 1) * 4) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+          }
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int k = 0; k < 16 * OS / 64; ++k) {
+            const int r = k * (64 / OS) + out_lane / OS, c = cw + o + out_lane % OS * 8;
+            const int64_t row = here.r0 + wm * CM + 16 * j + r;
+            const uint4 v = *reinterpret_cast<const uint4*>(tile + r * OC + ((out_lane % OS) ^ (r & (OS - 1))) * 8);
+            if (row < a.rows && c < a.n) *reinterpret_cast<uint4*>(a.out + row * a.n + c) = v;
+          }
+          __builtin_amdgcn_wave_barrier();
+        }
     }
+    if (id + (int)gridDim.x < total) here = tile_of<TN, TM>(g, blocks, id + gridDim.x);
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (what is behind the stream's end has to be in this block's LDS before that is another's)
 }
 
 // the parts' sums, in their order
@@ -318,26 +468,30 @@ __global__ __launch_bounds__(256) void proj_join_kernel(ProjMatmul a, int splits
 constexpr int CUS = 256;
 
 struct Plan {
-  int few, nt, nw;            // rows of 16, columns of 16 a wave, waves; or
+  int few, nt, nw, pd;        // rows of 16, columns of 16 a wave, waves, stages; or
   int tile;                   // of many: columns and rows
   Tiles g;
 };
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
+// columns and rows of a tile, blocks a compute unit
+constexpr struct { int tn, tm, slots; } TILES[] = {{64, 32, 2}, {64, 64, 2}, {128, 128, 2}, {256, 256, 1}, {128, 64, 2}, {128, 32, 2}, {128, 128, 1}, {64, 128, 2}};
+
 Plan plan_of(int rows, int n, int cols) {
   Plan p{};
   const int blocks = blocks_of(cols);
-  const int few_max = knob("FKV_FEW", 64);
-  if (rows <= few_max && rows <= 64) {
-    p.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.nt = knob("FKV_NT", 2);
+  const int few_max = knob("FKV_FEW", 16);
+  if (rows <= few_max && rows <= 32) {
+    p.few = rows <= 16 ? 1 : 2;
+    p.nt = knob("FKV_NT", 1);
     p.nw = knob("FKV_NW", 8);
+    p.pd = knob("FKV_PD", 2);
     return p;
   }
-  p.tile = knob("FKV_TILE", (int64_t)ceil_div(n, 256) * ceil_div(rows, 256) >= CUS ? 256 : 128);
-  p.g.tn = ceil_div(n, p.tile);
-  p.g.tm = ceil_div(rows, p.tile);
-  const int64_t tiles = (int64_t)p.g.tn * p.g.tm, slots = p.tile == 256 ? CUS : 2 * CUS;
+  p.tile = knob("FKV_TILE", rows <= 32 ? 0 : rows <= 64 ? 1 : (int64_t)ceil_div(n, 256) * ceil_div(rows, 256) >= CUS ? 3 : 2);
+  p.g.tn = ceil_div(n, TILES[p.tile].tn);
+  p.g.tm = ceil_div(rows, TILES[p.tile].tm);
+  const int64_t tiles = (int64_t)p.g.tn * p.g.tm, slots = TILES[p.tile].slots * CUS;
   int splits = knob("FKV_SPLITS", 0);
   if (!splits) splits = (int)(tiles * 2 <= slots ? slots / tiles : 1);
   if (splits > blocks / 4) splits = blocks / 4 > 0 ? blocks / 4 : 1;
@@ -357,25 +511,41 @@ void launch_proj_matmul(int dtype, const ProjMatmul& a, hipStream_t st) {
   const Plan p = plan_of(a.rows, a.n, a.cols);
   auto go = [&](auto dt) {
     if (p.few) {
-      auto few = [&](auto mt, auto nt, auto nw) {
-        hipLaunchKernelGGL((proj_few_kernel<dt(), mt(), nt(), nw()>), dim3((uint32_t)ceil_div(a.n, 16 * nt())), dim3(nw() * 64), 0, st, a);
+      auto few = [&](auto mt, auto nt, auto nw, auto pd) {
+        hipLaunchKernelGGL((proj_few_kernel<dt(), mt(), nt(), nw(), pd()>), dim3((uint32_t)ceil_div(a.n, 16 * nt())), dim3(nw() * 64), 0, st, a);
       };
-      auto few_m = [&](auto nt, auto nw) {
-        if (p.few == 1) few(std::integral_constant<int, 1>(), nt, nw);
-        else if (p.few == 2) few(std::integral_constant<int, 2>(), nt, nw);
-        else few(std::integral_constant<int, 4>(), nt, nw);
+#define C(x) std::integral_constant<int, x>()
+      auto few_m = [&](auto nt, auto nw, auto pd) {
+        if (p.few == 1) few(C(1), nt, nw, pd);
+        else if constexpr ((nt() + 2) * nw() * pd() <= 70) few(C(2), nt, nw, pd);
       };
-      if (p.nt == 1 && p.nw == 8) few_m(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
-      else if (p.nt == 1 && p.nw == 4) few_m(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
-      else if (p.nt == 1 && p.nw == 16) few_m(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
-      else if (p.nw == 4) few_m(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
-      else few_m(std::integral_constant<int, 2>(), std::integral_constant<int, 8>());
+      const int v = p.nt * 10000 + p.nw * 100 + p.pd;
+      if (v == 10802) few_m(C(1), C(8), C(2));
+#ifdef FKV_EXPERIMENT_KNOBS
+      if (v == 10404) few_m(C(1), C(4), C(4));
+      if (v == 10803) few_m(C(1), C(8), C(3));
+      if (v == 10804) few_m(C(1), C(8), C(4));
+      if (v == 10402) few_m(C(1), C(4), C(2));
+      if (v == 11602) few_m(C(1), C(16), C(2));
+      if (v == 20402) few_m(C(2), C(4), C(2));
+      if (v == 20403) few_m(C(2), C(4), C(3));
+      if (v == 20802) few_m(C(2), C(8), C(2));
+      if (v == 20803) few_m(C(2), C(8), C(3));
+#endif
       return;
     }
-    const dim3 grid((uint32_t)(p.g.tn * p.g.tm * p.g.splits));
+    const dim3 grid((uint32_t)std::min((int64_t)p.g.tn * p.g.tm * p.g.splits, (int64_t)TILES[p.tile].slots * CUS));
     auto many = [&](auto split) {
-      if (p.tile == 256) hipLaunchKernelGGL((proj_many_kernel<dt(), 256, 256, 2, 4, split()>), grid, dim3(512), 0, st, a, p.g);
-      else hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, split()>), grid, dim3(256), 0, st, a, p.g);
+      if (p.tile == 3) hipLaunchKernelGGL((proj_many_kernel<dt(), 256, 256, 2, 4, 2, 4, split()>), grid, dim3(512), 0, st, a, p.g);
+      else if (p.tile == 2) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, 2, 4, split()>), grid, dim3(256), 0, st, a, p.g);
+      else if (p.tile == 1) hipLaunchKernelGGL((proj_many_kernel<dt(), 64, 64, 2, 2, 4, 16, split()>), grid, dim3(256), 0, st, a, p.g);
+      else if (p.tile == 0) hipLaunchKernelGGL((proj_many_kernel<dt(), 64, 32, 2, 2, 5, 16, split()>), grid, dim3(256), 0, st, a, p.g);
+#ifdef FKV_EXPERIMENT_KNOBS
+      else if (p.tile == 4) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 64, 4, 1, 3, 16, split()>), grid, dim3(256), 0, st, a, p.g);
+      else if (p.tile == 5) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 32, 4, 1, 3, 16, split()>), grid, dim3(256), 0, st, a, p.g);
+      else if (p.tile == 6) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, 4, 8, split()>), grid, dim3(256), 0, st, a, p.g);
+      else if (p.tile == 7) hipLaunchKernelGGL((proj_many_kernel<dt(), 64, 128, 2, 2, 3, 8, split()>), grid, dim3(256), 0, st, a, p.g);
+#endif
     };
     if (p.g.splits == 1) return many(std::false_type());
     many(std::true_type());
