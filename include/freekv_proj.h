@@ -53,10 +53,10 @@ int fkv_proj_rope(int32_t device, int32_t dtype, const void* qkv_dev, int32_t ro
 
 /* out[r, c] = T(sum_b scale_x[r, b] scale_w[c / 128, b] sum_{i in block b} x[r, i] w[c, i]):
  * x codes [rows, cols] with a scale for each row's block, w codes [n, cols] with one for each 128 x 128, out [rows, n] of T, n: 1 to 4194304,
- * rows times n at most 2^37.  Sums are in fp32, their order is fixed by the sizes.  Up to 64 rows the products that they are of are exact; beyond, the 8-bit
+ * rows times n at most 2^37.  Sums are in fp32, their order is fixed by the sizes.  Up to 32 rows the products that they are of are exact; beyond, the 8-bit
  * matrix instruction cuts products at 2^-13 of the largest of eight adjacent columns before it adds them.  Where the product of two scales is below 2^-126
  * digits are lost, beyond fp32's largest it is infinite (NaN where it meets a sum of 0).
- * work_dev: at least fkv_proj_workspace's bytes, this call's until the stream is done with it; NULL where they are 0, as they are up to 64 rows. */
+ * work_dev: at least fkv_proj_workspace's bytes, this call's until the stream is done with it; NULL where they are 0, as they are up to 32 rows. */
 int fkv_proj_matmul(int32_t device, int32_t dtype, const void* x_dev, const float* x_scales_dev, const void* w_dev, const float* w_scales_dev, int32_t rows,
                     int32_t n, int32_t cols, void* out_dev, void* work_dev, size_t work_bytes, void* stream);
 int fkv_proj_workspace(int32_t rows, int32_t n, int32_t cols, size_t* work_bytes);

@@ -193,7 +193,7 @@ struct Tile {
   int split, c0, b0, b1;
   int64_t r0;
 };
-// Tiles dealt to the XCDs in runs (blocks go to them in turn); within a run eight tiles of rows, then the next of columns.
+// Tiles dealt to the XCDs in runs (blocks go to them in turn); within a run four tiles of rows, then the next of columns.
 template <int TN, int TM>
 __device__ __forceinline__ Tile tile_of(const Tiles& g, int blocks, int id) {
   const int total = g.tn * g.tm * g.splits, each = total / 8, more = total % 8, x = id % 8;
@@ -201,7 +201,7 @@ __device__ __forceinline__ Tile tile_of(const Tiles& g, int blocks, int id) {
   Tile t;
   t.split = id / (g.tn * g.tm);
   id -= t.split * (g.tn * g.tm);
-  const int group = 8 * g.tn, first = id / group * 8, high = min(8, g.tm - first);
+  const int group = 4 * g.tn, first = id / group * 4, high = min(4, g.tm - first);
   t.r0 = (int64_t)(first + (id % group) % high) * TM;
   t.c0 = (id % group) / high * TN;
   t.b0 = t.split * g.per;
@@ -211,15 +211,14 @@ __device__ __forceinline__ Tile tile_of(const Tiles& g, int blocks, int id) {
 
 // SB: blocks of 128 whose scales go through LDS at a time
 template <int DT, int TN, int TM, int WN, int WM, int ST, int SB, bool SPLIT>
-__global__ __launch_bounds__(WN * WM * 64) void proj_many_kernel(ProjMatmul a, Tiles g) {
+__global__ __launch_bounds__(WN * WM * 64, 2) void proj_many_kernel(ProjMatmul a, Tiles g) {
   constexpr int NW = WN * WM, CN = TN / WN, CM = TM / WM, AN = CN / 16, AM = CM / 16, ROWS = TN + TM, LOADS = ROWS / 8 / NW;
-  constexpr int WB = (TN + QB - 1) / QB, SE = TM * SB / (NW * 64);             // blocks of weights, scales a thread
-  constexpr int OC = CN < 64 ? CN : 64, OS = OC / 8;                           // columns of results on their way out, and 16-byte parts of a row
-  constexpr bool EARLY = ST == 2;                                              // a stage is filled again before its products are done
-  static_assert(ROWS % (8 * NW) == 0 && TN % (8 * NW) == 0 && CN <= QB && QB % CN == 0 && AN % 2 == 0 && ST >= 2 && (!EARLY || AN >= 4), "");
-  static_assert(SE >= 1 && SE <= SB && SE * NW * 64 == TM * SB && SB * WB <= NW * 64, "");
+  constexpr int WB = (TN + QB - 1) / QB, SL = TM * SB / 64 / NW;               // blocks of weights; loads of scales
+  constexpr int OC = 32, OS = OC / 8;                                          // columns of results on their way out, and 16-byte parts of a row
+  static_assert(ROWS % (8 * NW) == 0 && TN % (8 * NW) == 0 && CN <= QB && QB % CN == 0 && AN >= 4 && AN % 4 == 0 && ST >= 2, "");
+  static_assert(SL * NW * 64 == TM * SB && SB * WB <= 64 && 64 % SB == 0 && CN % OC == 0, "");
   __shared__ __attribute__((aligned(1024))) uint8_t s_tile[ST][ROWS * QB];
-  __shared__ float s_xs[2][SB][TM], s_ws[2][SB][WB];
+  __shared__ float s_xs[2][TM][SB], s_ws[2][64];                               // (the weights': [block of rows][SB])
   __shared__ __attribute__((aligned(16))) uint16_t s_out[SPLIT ? 1 : NW][16 * OC];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, gr = lane >> 4;
   const int wn = wave % WN, wm = wave / WN, total = g.tn * g.tm * g.splits, blocks = blocks_of(a.cols);
@@ -254,31 +253,27 @@ __global__ __launch_bounds__(WN * WM * 64) void proj_many_kernel(ProjMatmul a, T
     const bool is_w = r < TN;
     load_lds(is_w ? wbuf : xbuf, off + (uint32_t)(r - (is_w ? 0 : TN)) * (uint32_t)a.cols, lds_of(s_tile) + slot * (ROWS * QB) + (r + wave * 8) * QB);
   };
-  // Scales of SB blocks at a time: a row's lie behind each other in memory and are wanted row by row.
-  float scales[SE + 1];
-  int sid = blockIdx.x, sb = here.b0, sb_end = here.b1, sc0 = here.c0;
-  int64_t sr0 = here.r0;
-  auto scales_from = [&]() {
-    if (sb >= sb_end) {
+  // Scales go through LDS in runs of SB blocks, whole runs ahead: a row's lie behind each other in memory.
+  Tile st = here;
+  int sid = blockIdx.x, sb = here.b0;
+  auto scales = [&](int which) {
+    if (sb >= st.b1) {
       sid += gridDim.x;
-      if (sid >= total) return;
-      const Tile to = tile_of<TN, TM>(g, blocks, sid);
-      sb = to.b0, sb_end = to.b1, sc0 = to.c0, sr0 = to.r0;
+      if (sid < total) st = tile_of<TN, TM>(g, blocks, sid), sb = st.b0;
     }
-    const uint32_t tid = wave * 64 + anew(lane);
-    const int e = tid % (SB / SE) * SE, r = min((int64_t)(tid / (SB / SE)), a.rows - 1 - sr0);
-    const float* p = a.xs + sr0 * blocks;
+    if (sid >= total) return;
+    const int4v xs = buffer_of((const uint8_t*)(a.xs + st.r0 * blocks), (uint32_t)min((int64_t)TM, a.rows - st.r0) * (uint32_t)blocks * 4u);
+    const uint32_t l = anew(lane);
 #pragma unroll
-    for (int k = 0; k < SE; ++k) scales[k] = p[(uint32_t)(r * blocks + min(sb + e + k, blocks - 1))];
-    const int wb = min(tid < SB * WB ? (int)tid / SB : 0, blocks_of(a.n) - 1 - sc0 / QB);
-    scales[SE] = (a.ws + (int64_t)(sc0 / QB) * blocks)[(uint32_t)(wb * blocks + min(sb + (int)tid % SB, blocks - 1))];
+    for (int i = 0; i < SL; ++i) {
+      const int r = (i * NW + wave) * (64 / SB);
+      load_lds4(xs, ((r + l / SB) * blocks + sb + l % SB) * 4u, lds_of(&s_xs[which][r][0]));
+    }
+    if (wave == 0) {
+      const int4v ws = buffer_of((const uint8_t*)(a.ws + (int64_t)(st.c0 / QB) * blocks), (uint32_t)min(WB, blocks_of(a.n) - st.c0 / QB) * (uint32_t)blocks * 4u);
+      load_lds4(ws, (l / SB * blocks + sb + l % SB) * 4u, lds_of(&s_ws[which][0]));
+    }
     sb += SB;
-  };
-  auto scales_to = [&](int which) {
-    const uint32_t tid = wave * 64 + anew(lane);
-#pragma unroll
-    for (int k = 0; k < SE; ++k) s_xs[which][tid % (SB / SE) * SE + k][tid / (SB / SE)] = scales[k];
-    if (tid < SB * WB) s_ws[which][tid % SB][tid / SB] = scales[SE];
   };
 
   const int lo = t * QB + ((gr ^ (t & 7)) * 16), hi = lo ^ 64;
@@ -291,30 +286,36 @@ __global__ __launch_bounds__(WN * WM * 64) void proj_many_kernel(ProjMatmul a, T
   auto row_x = [&](int j) { return TN + wm * CM + 16 * j; };
 
   // Loads are asked for one at a time between the products: a wave that asks for many at once waits for room in the queue.
-  // With two stages there is one meeting a block, before the last two steps.  By then every wave has this block's operands and what it asked for
-  // of the next, so the rest of the products cover the first operands of the next block, and the next but one is asked for: LOADS / 2 now, the
-  // others in the first steps of the next block.
+  // There is one meeting a block, before the last two steps.  By then every wave has this block's operands and what it asked for of the next
+  // one, so the rest of the products cover the next block's first operands, and the stage is filled again: LOADS / 2 loads now, the others
+  // in the first steps of the next block.
   constexpr int NA = LOADS / 2;
-  scales_from();
+  scales(0);
+  scales(1);
 #pragma unroll
-  for (int st = 0; st < ST - 1; ++st) {
+  for (int i = 0; i < ST - 1; ++i) {
     begin();
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) bring(i);
+    for (int k = 0; k < LOADS; ++k) bring(k);
   }
-  scales_to(0);
+  // loads end in order: what was asked for behind a stage may still be on its way
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((ST - 2) * LOADS) : "memory");
+  begin();
+#pragma unroll
+  for (int i = 0; i < NA; ++i) bring(i);
   word8 xv[AM], wv[4];
-  if (EARLY) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    begin();
+  wv[0] = operand(0, row_w(0));
+  wv[1] = operand(0, row_w(1));
 #pragma unroll
-    for (int i = 0; i < NA; ++i) bring(i);
-    wv[0] = operand(0, row_w(0));
-    wv[1] = operand(0, row_w(1));
+  for (int j = 0; j < AM; ++j) xv[j] = operand(0, row_x(j));
+  int stage = 0, which = 0, nth = 0;                       // of the scales: the run's place, and the block's in it
+  float s_next[AM], ws_next;
+  auto next_scales = [&]() {
+    ws_next = s_ws[which][wn * CN / QB * SB + nth];
 #pragma unroll
-    for (int j = 0; j < AM; ++j) xv[j] = operand(0, row_x(j));
-  }
-  int stage = 0, which = 0;
+    for (int j = 0; j < AM; ++j) s_next[j] = s_xs[which][wm * CM + 16 * j + t][nth];
+  };
+  next_scales();
   for (int id = blockIdx.x; id < total; id += gridDim.x) {
     float4v acc[AN][AM], p[AM];
     float s[AM], s_before[AM];
@@ -335,65 +336,51 @@ __global__ __launch_bounds__(WN * WM * 64) void proj_many_kernel(ProjMatmul a, T
       p[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[i % 4], xv[j], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     };
-    int nth = 0;
     for (int b = here.b0; b < here.b1; ++b) {
       const bool last = nth == SB - 1 || b + 1 == here.b1;
-      if (!EARLY) {
-        // loads end in order: what was asked for behind this stage may still be on its way
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((ST - 2) * LOADS) : "memory");
-        wv[0] = operand(stage, row_w(0));
 #pragma unroll
-        for (int j = 0; j < AM; ++j) xv[j] = operand(stage, row_x(j));
-        wv[1] = operand(stage, row_w(1));
-      }
-      const float ws = s_ws[which][nth][wn * CN / QB];
+      for (int i = 0; i < AN - 2; ++i) {
+        if (i == 1)
 #pragma unroll
-      for (int j = 0; j < AM; ++j) s[j] = s_xs[which][nth][wm * CM + 16 * j + t] * ws;
-      if (!EARLY && last && nth) scales_to(which ^ 1);
-      if (nth == 0) scales_from();
-      if (!EARLY && last && !nth) scales_to(which ^ 1);
-      if (!EARLY) begin();
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < (EARLY ? AN - 2 : AN); ++i) {
-        if (i + 2 < AN) wv[(i + 2) % 4] = operand(stage, row_w(i + 2));
+          for (int j = 0; j < AM; ++j) s[j] = s_next[j] * ws_next;
+        wv[(i + 2) % 4] = operand(stage, row_w(i + 2));
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < AM; ++j) {
           multiply(i, j);
-          // (its place among the loads: of the first two steps, or of all)
-          constexpr int PLACES = EARLY ? 2 * AM : AN * AM, N = EARLY ? LOADS - NA : LOADS;
+          constexpr int PLACES = 2 * AM, N = LOADS - NA;
           const int at = i * AM + j;
           if (at < PLACES)
 #pragma unroll
-            for (int k = at * N / PLACES; k < (at + 1) * N / PLACES; ++k) bring(EARLY ? NA + k : k);
+            for (int k = at * N / PLACES; k < (at + 1) * N / PLACES; ++k) bring(NA + k);
         }
       }
       stage = stage + 1 < ST ? stage + 1 : 0;
-      if (EARLY) {
-        if (last) scales_to(which ^ 1);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        begin();
-        wv[0] = operand(stage, row_w(0));
-        wv[1] = operand(stage, row_w(1));
-        __builtin_amdgcn_sched_barrier(0);
+      // (the next run's scales were asked for at the end of the one before this: too few loads ago where this one is short)
+      if (ST > 2 && last && nth < ST - 3) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((ST - 2) * LOADS) : "memory");
+      if (last) scales(which);
+      begin();
+      nth = last ? 0 : nth + 1;
+      which ^= last;
+      wv[0] = operand(stage, row_w(0));
+      wv[1] = operand(stage, row_w(1));
+      next_scales();
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j <= AM; ++j) {
-          if (j < AM) multiply(AN - 2, j);
-          if (j) {
-            multiply(AN - 1, j - 1);
-            xv[j - 1] = operand(stage, row_x(j - 1));
-          }
-          if (j < AM)
-#pragma unroll
-            for (int k = j * NA / AM; k < (j + 1) * NA / AM; ++k) bring(k);
-          __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j <= AM; ++j) {
+        if (j < AM) multiply(AN - 2, j);
+        if (j) {
+          multiply(AN - 1, j - 1);
+          xv[j - 1] = operand(stage, row_x(j - 1));
         }
+        if (j < AM)
+#pragma unroll
+          for (int k = j * NA / AM; k < (j + 1) * NA / AM; ++k) bring(k);
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int j = 0; j < AM; ++j) s_before[j] = s[j];
-      nth = last ? 0 : nth + 1;
-      which ^= last;
     }
 #pragma unroll
     for (int j = 0; j < AM; ++j)
@@ -468,35 +455,53 @@ __global__ __launch_bounds__(256) void proj_join_kernel(ProjMatmul a, int splits
 constexpr int CUS = 256;
 
 struct Plan {
-  int few, nt, nw, pd;        // rows of 16, columns of 16 a wave, waves, stages; or
-  int tile;                   // of many: columns and rows
+  bool few;
+  int nt, nw;                 // of few rows: tiles of 16 columns, waves
+  int tile;                   // of many
   Tiles g;
 };
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// columns and rows of a tile, blocks a compute unit
-constexpr struct { int tn, tm, slots; } TILES[] = {{64, 32, 2}, {64, 64, 2}, {128, 128, 2}, {256, 256, 1}, {128, 64, 2}, {128, 32, 2}, {128, 128, 1}, {64, 128, 2}};
+// The tiles that many rows are cut into, and what they cost, in us: a block of 128 columns where a compute unit has one of them and where it has
+// two, and a tile's results.  From products of 48 to 1024 rows (n x cols of 4096 x 11056 and x 14336, 6144 and 28672 x 4096, 8192 x 8192,
+// 1 to 16 parts), whose times these give within 8 %.
+constexpr struct { int tn, tm, slots; float one, two, results; } TILES[] = {
+    {64, 64, 2, 0.40f, 0.58f, 0.f}, {128, 128, 1, 0.76f, 0.76f, 2.f}, {128, 128, 2, 1.38f, 1.45f, 1.f}, {256, 256, 1, 2.0f, 2.0f, 0.f}};
+constexpr float READ_RATE = 4.5e6f, JOIN = 3.f, JOIN_RATE = 7.5e6f;       // bytes a us of weights, us of a join's launch, bytes a us of parts
+constexpr int MAX_PARTS = 16, LEAST_PART = 4;
 
+// Up to 32 rows the weights' bytes are what counts, beyond it is tiles.  32 rows x 28672 x 4096: 34 us, as tiles 33; 32 x 6144 x 4096: 9.1 and 12.2;
+// 48 rows as tiles 34 and 13.4, three tiles of 16 rows at a time 57 and 18.
+// Few rows: two tiles of 16 columns to a block, as its waves read all activations (16 rows x 28672 x 4096 26.3 us, one 28.2), but where that
+// leaves compute units without a block and each wave much to read (16 rows x 4096 x 14336: 14.7 us, one tile and eight waves 12.2).
 Plan plan_of(int rows, int n, int cols) {
   Plan p{};
   const int blocks = blocks_of(cols);
-  const int few_max = knob("FKV_FEW", 16);
-  if (rows <= few_max && rows <= 32) {
-    p.few = rows <= 16 ? 1 : 2;
-    p.nt = knob("FKV_NT", 1);
-    p.nw = knob("FKV_NW", 8);
-    p.pd = knob("FKV_PD", 2);
+  if (rows <= 32) {
+    p.few = true;
+    const bool narrow = ceil_div(n, 32) < CUS && blocks > 48;
+    p.nt = narrow ? 1 : 2;
+    p.nw = narrow ? 8 : 4;
     return p;
   }
-  p.tile = knob("FKV_TILE", rows <= 32 ? 0 : rows <= 64 ? 1 : (int64_t)ceil_div(n, 256) * ceil_div(rows, 256) >= CUS ? 3 : 2);
-  p.g.tn = ceil_div(n, TILES[p.tile].tn);
-  p.g.tm = ceil_div(rows, TILES[p.tile].tm);
-  const int64_t tiles = (int64_t)p.g.tn * p.g.tm, slots = TILES[p.tile].slots * CUS;
-  int splits = knob("FKV_SPLITS", 0);
-  if (!splits) splits = (int)(tiles * 2 <= slots ? slots / tiles : 1);
-  if (splits > blocks / 4) splits = blocks / 4 > 0 ? blocks / 4 : 1;
-  p.g.per = ceil_div(blocks, splits);
-  p.g.splits = ceil_div(blocks, p.g.per);
+  float best = 0.f;
+  for (int t = 0; t < (int)(sizeof(TILES) / sizeof(TILES[0])); ++t) {
+    const int tn = ceil_div(n, TILES[t].tn), tm = ceil_div(rows, TILES[t].tm), slots = TILES[t].slots * CUS;
+    for (int k = 1; k <= MAX_PARTS; ++k) {
+      if (k > 1 && blocks < k * LEAST_PART) break;
+      const int per = ceil_div(blocks, k), splits = ceil_div(blocks, per);
+      const int64_t work = (int64_t)tn * tm * splits, rounds = work / slots, rest = work % slots;
+      float us = rounds * (per * (slots > CUS ? TILES[t].two : TILES[t].one) + TILES[t].results);
+      if (rest) us += per * (rest > CUS ? TILES[t].two : TILES[t].one) + TILES[t].results;
+      us = std::max(us, (float)n * cols / READ_RATE);
+      if (splits > 1) us += JOIN + 8.f * splits * rows * n / JOIN_RATE;
+      if (best == 0.f || us < best) best = us, p.tile = t, p.g = {tn, tm, splits, per};
+    }
+  }
+  if (const int t = knob("FKV_TILE", -1); t >= 0) {
+    const int k = knob("FKV_SPLITS", 1), per = ceil_div(blocks, k);
+    p.tile = t, p.g = {ceil_div(n, TILES[t].tn), ceil_div(rows, TILES[t].tm), ceil_div(blocks, per), per};
+  }
   return p;
 }
 
@@ -504,48 +509,26 @@ Plan plan_of(int rows, int n, int cols) {
 
 size_t proj_matmul_work(int rows, int n, int cols) {
   const Plan p = plan_of(rows, n, cols);
-  return !p.few && p.g.splits > 1 ? (size_t)p.g.splits * rows * ((n + 3) / 4 * 4) * 4 : 0;
+  return p.g.splits > 1 ? (size_t)p.g.splits * rows * ((n + 3) / 4 * 4) * 4 : 0;
 }
 
 void launch_proj_matmul(int dtype, const ProjMatmul& a, hipStream_t st) {
   const Plan p = plan_of(a.rows, a.n, a.cols);
   auto go = [&](auto dt) {
     if (p.few) {
-      auto few = [&](auto mt, auto nt, auto nw, auto pd) {
-        hipLaunchKernelGGL((proj_few_kernel<dt(), mt(), nt(), nw(), pd()>), dim3((uint32_t)ceil_div(a.n, 16 * nt())), dim3(nw() * 64), 0, st, a);
-      };
-#define C(x) std::integral_constant<int, x>()
-      auto few_m = [&](auto nt, auto nw, auto pd) {
-        if (p.few == 1) few(C(1), nt, nw, pd);
-        else if constexpr ((nt() + 2) * nw() * pd() <= 70) few(C(2), nt, nw, pd);
-      };
-      const int v = p.nt * 10000 + p.nw * 100 + p.pd;
-      if (v == 10802) few_m(C(1), C(8), C(2));
-#ifdef FKV_EXPERIMENT_KNOBS
-      if (v == 10404) few_m(C(1), C(4), C(4));
-      if (v == 10803) few_m(C(1), C(8), C(3));
-      if (v == 10804) few_m(C(1), C(8), C(4));
-      if (v == 10402) few_m(C(1), C(4), C(2));
-      if (v == 11602) few_m(C(1), C(16), C(2));
-      if (v == 20402) few_m(C(2), C(4), C(2));
-      if (v == 20403) few_m(C(2), C(4), C(3));
-      if (v == 20802) few_m(C(2), C(8), C(2));
-      if (v == 20803) few_m(C(2), C(8), C(3));
-#endif
+      const dim3 grid((uint32_t)ceil_div(a.n, 16 * p.nt)), block((uint32_t)p.nw * 64);
+      if (p.nt == 1 && a.rows <= 16) hipLaunchKernelGGL((proj_few_kernel<dt(), 1, 1, 8, 2>), grid, block, 0, st, a);
+      else if (p.nt == 1) hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 1, 8, 2>), grid, block, 0, st, a);
+      else if (a.rows <= 16) hipLaunchKernelGGL((proj_few_kernel<dt(), 1, 2, 4, 2>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 2, 4, 2>), grid, block, 0, st, a);
       return;
     }
     const dim3 grid((uint32_t)std::min((int64_t)p.g.tn * p.g.tm * p.g.splits, (int64_t)TILES[p.tile].slots * CUS));
     auto many = [&](auto split) {
-      if (p.tile == 3) hipLaunchKernelGGL((proj_many_kernel<dt(), 256, 256, 2, 4, 2, 4, split()>), grid, dim3(512), 0, st, a, p.g);
-      else if (p.tile == 2) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, 2, 4, split()>), grid, dim3(256), 0, st, a, p.g);
-      else if (p.tile == 1) hipLaunchKernelGGL((proj_many_kernel<dt(), 64, 64, 2, 2, 4, 16, split()>), grid, dim3(256), 0, st, a, p.g);
-      else if (p.tile == 0) hipLaunchKernelGGL((proj_many_kernel<dt(), 64, 32, 2, 2, 5, 16, split()>), grid, dim3(256), 0, st, a, p.g);
-#ifdef FKV_EXPERIMENT_KNOBS
-      else if (p.tile == 4) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 64, 4, 1, 3, 16, split()>), grid, dim3(256), 0, st, a, p.g);
-      else if (p.tile == 5) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 32, 4, 1, 3, 16, split()>), grid, dim3(256), 0, st, a, p.g);
-      else if (p.tile == 6) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, 4, 8, split()>), grid, dim3(256), 0, st, a, p.g);
-      else if (p.tile == 7) hipLaunchKernelGGL((proj_many_kernel<dt(), 64, 128, 2, 2, 3, 8, split()>), grid, dim3(256), 0, st, a, p.g);
-#endif
+      if (p.tile == 0) hipLaunchKernelGGL((proj_many_kernel<dt(), 64, 64, 1, 4, 4, 16, split()>), grid, dim3(256), 0, st, a, p.g);
+      else if (p.tile == 1) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, 4, 16, split()>), grid, dim3(256), 0, st, a, p.g);
+      else if (p.tile == 2) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, 2, 8, split()>), grid, dim3(256), 0, st, a, p.g);
+      else hipLaunchKernelGGL((proj_many_kernel<dt(), 256, 256, 2, 4, 2, 8, split()>), grid, dim3(512), 0, st, a, p.g);
     };
     if (p.g.splits == 1) return many(std::false_type());
     many(std::true_type());

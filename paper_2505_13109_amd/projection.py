@@ -16,7 +16,7 @@ import torch
 from .binding import FreeKVError, lib
 
 BLOCK = 128
-FEW_ROWS = 16                 # up to here a product needs no workspace
+FEW_ROWS = 32                 # up to here a product needs no workspace
 CODES = torch.float8_e4m3fn
 _TYPES = {torch.float16: 0, torch.bfloat16: 1}
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None

@@ -321,7 +321,7 @@ def product(x, xs, w, ws, dtype):
     return out
 
 
-FEW = 16               # rows up to which no product is cut
+FEW = 32               # rows up to which no product is cut
 
 
 # 128 products a block and the blocks' sums, each addition off by a step of fp32 of the terms' sizes at most, and the scales' product and its own
