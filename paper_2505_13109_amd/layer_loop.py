@@ -16,6 +16,9 @@ would not produce.
 Over a `PagedCache` the stack decodes the sequences `seqs` (int32 slots on the GPU) of any lengths: every layer appends its keys and
 values to the 4-bit cache and attends over all of it.  Lengths, and with them the rotary positions, stay on the device, so
 `step()` may be captured into a graph and every replay decodes the next token.
+
+With `weights="fp8"` the weights are kept in 8 bits and everything around the loop runs in the library's own kernels (`projection.py`): the
+residual's addition with the norm, the products, rotary positions, the gated activation.  Rotary positions may then have several axes.
 """
 from __future__ import annotations
 
@@ -23,12 +26,18 @@ import torch
 
 from .binding import FreeKV
 from .paged_cache import PagedCache
+from .projection import empty_quant, proj_gate, proj_matmul, proj_norm, proj_quant, proj_rope
 
 
 class DecoderStack:
     def __init__(self, fkv: FreeKV | PagedCache, *, seqs: torch.Tensor | None = None, ffn_mult: float = 3.5, seed: int = 7, rope_base: float = 500000.0,
-                 copy_stream: torch.cuda.Stream | None = None):
+                 copy_stream: torch.cuda.Stream | None = None, weights: str | None = None, rope_sections=None):
+        """weights: None, the storage type's 16 bits, or "fp8".  rope_sections (fp8 only): `proj_rope`'s, for positions of several axes."""
         c = fkv.cfg
+        if weights not in (None, "fp8"):
+            raise ValueError(f"weights: None or 'fp8' are known, not {weights!r}")
+        if rope_sections is not None and weights is None:
+            raise ValueError("positions of several axes go with weights='fp8'")
         self.fkv, self.seqs = fkv, seqs
         self.paged = isinstance(fkv, PagedCache)
         if self.paged != (seqs is not None):
@@ -46,16 +55,36 @@ class DecoderStack:
 
         qkv_out = (self.n_q + 2 * self.n_kv) * self.d
         s_in = self.hidden ** -0.5
-        self.wqkv = [mk(self.hidden, qkv_out, scale=s_in) for _ in range(self.n_layers)]
-        self.wo = [mk(self.hidden, self.hidden, scale=s_in) for _ in range(self.n_layers)]
-        self.wgu = [mk(self.hidden, 2 * self.ffn, scale=s_in) for _ in range(self.n_layers)]
-        self.wd = [mk(self.ffn, self.hidden, scale=self.ffn ** -0.5) for _ in range(self.n_layers)]
+        keep = (lambda w: w) if weights is None else self._in_8_bits
+        if weights is not None and self.ffn % 16:
+            raise ValueError(f"weights='fp8' wants a multiple of 16 for the FFN's width, {ffn_mult} x {self.hidden} gives {self.ffn}")
+        self.wqkv = [keep(mk(self.hidden, qkv_out, scale=s_in)) for _ in range(self.n_layers)]
+        self.wo = [keep(mk(self.hidden, self.hidden, scale=s_in)) for _ in range(self.n_layers)]
+        self.wgu = [keep(mk(self.hidden, 2 * self.ffn, scale=s_in)) for _ in range(self.n_layers)]
+        self.wd = [keep(mk(self.ffn, self.hidden, scale=self.ffn ** -0.5)) for _ in range(self.n_layers)]
         self.inv_freq = (rope_base ** (-torch.arange(0, self.d, 2, device=dev, dtype=torch.float32) / self.d))
         self.out = torch.empty((self.n_layers, self.batch, self.n_q, self.d), dtype=self.dtype if self.paged else torch.float32, device=dev)
         self.lens = torch.zeros((self.batch,), dtype=torch.int32, device=dev)
         self.copy_stream = copy_stream
         self.last_qkv = [None] * self.n_layers       # what each layer fed to the loop at the last step (for tests)
-        self.weight_bytes_per_layer = (self.hidden * qkv_out + self.hidden * self.hidden + 3 * self.hidden * self.ffn) * 2
+        self.weight_bytes_per_layer = (self.hidden * qkv_out + self.hidden * self.hidden + 3 * self.hidden * self.ffn) * (2 if weights is None else 1)
+        self.weights, self.sections = weights, rope_sections
+        if weights is not None:
+            def new(*shape, dtype=self.dtype):
+                return torch.empty(shape, dtype=dtype, device=dev)
+
+            self.h8, self.f8 = (empty_quant(self.batch, cols, device=dev) for cols in (self.hidden, self.ffn))
+            self.qkv, self.gu, self.y = new(self.batch, qkv_out), new(self.batch, 2 * self.ffn), new(self.batch, self.hidden)
+            self.x = new(2, self.batch, self.hidden)         # the stream of a layer, before and behind the attention
+            self.heads = [tuple(new(self.batch, n, self.d) for n in (self.n_q, self.n_kv, self.n_kv)) for _ in range(self.n_layers)]
+            self.positions = new(self.batch, dtype=torch.int32)
+
+    @staticmethod
+    def _in_8_bits(w):
+        """[in, out] of the storage type -> codes [out, in] and a scale for each 128 x 128."""
+        codes, scales = empty_quant(w.shape[1], w.shape[0], tile=128, device=w.device)
+        proj_quant(w.T.contiguous(), codes, scales, tile=128)
+        return codes, scales
 
     def _rms(self, x):
         return torch.nn.functional.rms_norm(x, (self.hidden,), eps=1e-5)
@@ -65,18 +94,23 @@ class DecoderStack:
         a, b = x[..., : self.d // 2], x[..., self.d // 2:]
         return torch.cat([a * cos - b * sin, a * sin + b * cos], dim=-1)
 
-    def step(self, x, external_qkv=None, stream=None):
+    def step(self, x, external_qkv=None, stream=None, positions=None):
         """x [batch, hidden] -> [batch, hidden].  external_qkv: per layer (q [batch,n_q,d], k, v [batch,n_kv,d]).
+        positions (fp8 only): rotary positions of the tokens, [batch] or [axes, batch] int32 on the GPU; None: their places in the sequences, on
+        every axis.
 
         Over a PagedCache the whole step runs on `stream`, behind what the current stream has been given and before what it is given next:
         positions come from the device, so the projections have to follow the cache's calls.  Over a FreeKV context, `stream` is the one that
         its calls are launched on; the rest runs on the current stream, which has to be the same."""
+        if self.weights is None and positions is not None:
+            raise ValueError("positions of the caller's go with weights='fp8'")
+        run = self._step if self.weights is None else lambda *a: self._step_in_8_bits(*a, positions)
         here = torch.cuda.current_stream(self.fkv.device) if self.paged and stream is not None else None
         if here is None or stream == here:
-            return self._step(x, external_qkv, stream)
+            return run(x, external_qkv, stream)
         stream.wait_stream(here)
         with torch.cuda.stream(stream):
-            y = self._step(x, external_qkv, stream)
+            y = run(x, external_qkv, stream)
         here.wait_stream(stream)
         y.record_stream(here)
         return y
@@ -109,3 +143,43 @@ class DecoderStack:
             gu = self._rms(x) @ self.wgu[layer]
             x = x + (torch.nn.functional.silu(gu[:, : self.ffn]) * gu[:, self.ffn:]) @ self.wd[layer]
         return x
+
+    def _step_in_8_bits(self, x, external_qkv, stream, positions):
+        """The same step, the additions of a layer's two halves in the norms behind them."""
+        if self.paged:
+            self.fkv.extend(self.seqs, stream=stream)
+            self.fkv.tables(self.seqs, self.lens, stream=stream)
+        if positions is None:
+            places = self.lens - 1 if self.paged else torch.full_like(self.positions, self.fkv.context_len(0))
+            positions = places if self.sections is None else places.expand(1 + max(self._axes()), -1).contiguous()
+        y = None
+        for layer in range(self.n_layers):
+            if y is None:
+                proj_norm(x, None, *self.h8)
+            else:
+                proj_norm(x, None, *self.h8, add=y, res=self.x[0])
+                x = self.x[0]
+            proj_matmul(*self.h8, *self.wqkv[layer], self.qkv)
+            q, k, v = self.heads[layer]
+            proj_rope(self.qkv.view(self.batch, self.n_q + 2 * self.n_kv, self.d), positions, self.inv_freq, q, k, v, sections=self.sections)
+            if external_qkv is not None:
+                q, k, v = external_qkv[layer]
+            self.last_qkv[layer] = (q, k, v)
+            if self.paged:
+                self.fkv.append(layer, self.seqs, k, v, stream=stream)
+                self.fkv.attn(layer, self.seqs, q, self.out[layer], stream=stream)
+            else:
+                self.fkv.decode_step(layer, q, k, v, self.out[layer], stream=stream, copy_stream=self.copy_stream)
+            proj_quant(self.out[layer].to(self.dtype).view(self.batch, self.hidden), *self.h8)
+            proj_matmul(*self.h8, *self.wo[layer], self.y)
+            proj_norm(x, None, *self.h8, add=self.y, res=self.x[1])
+            x = self.x[1]
+            proj_matmul(*self.h8, *self.wgu[layer], self.gu)
+            proj_gate(self.gu, *self.f8)
+            proj_matmul(*self.f8, *self.wd[layer], self.y)
+            y = self.y
+        return x + y
+
+    def _axes(self):
+        s = list(self.sections)
+        return s if len(s) == 64 else range(len(s))
