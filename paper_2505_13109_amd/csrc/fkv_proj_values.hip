@@ -14,27 +14,31 @@ __device__ __forceinline__ uint4 load16(const uint16_t* p) { return *reinterpret
 
 // ---- plain values, and the gate: a thread one chunk of a row -------------------------------------------------
 
-// g / (1 + exp(-g)) u.  exp(-|g|) = 2^hi (1 + lo ln 2) with hi + lo = -|g| log2(e) to 48 bits; the product g u is exact for bf16, 22 of
-// 24 bits for fp16, so that what is left is about one rounding of the sigmoid and one of the result.
+// g / (1 + exp(-g)) u.  exp(-g) = 2^hi (1 + lo) with hi ln 2 + lo = -g to 48 bits; the reciprocal is the nearest but for its last
+// place, and the product g u is exact for bf16 and has 22 of 24 bits for fp16: about a rounding each for exp, sum, reciprocal and result.
+// (With exp(-|g|), a quotient and the sum's own rounding, nine more of 40 instructions a value: 4096 x 14336 73 us.)
 __device__ __forceinline__ float gated(float g, float u) {
-  const float a = -fabsf(g);
-  const float hi = a * 0x1.715476p+0f, lo = fmaf(a, 0x1.4ae0c0p-26f, fmaf(a, 0x1.715476p+0f, -hi));
-  const float p = __builtin_amdgcn_exp2f(hi);
-  const float t = fmaf(p, lo * 0x1.62e430p-1f, p);
-  const float d = 1.f + t, y = __builtin_amdgcn_rcpf(d);
-  const float n = g < 0.f ? t : 1.f;
-  // n / d from the reciprocal: the remainder counts what d was rounded by, too
-  const float s = n * y, rem = fmaf(-s, d, n) - s * (t - (d - 1.f));
-  return g * u * fmaf(rem, y, s);
+  const float hi = g * -0x1.715476p+0f, lo = fmaf(hi, 0x1.05c610p-29f, fmaf(hi, -0x1.62e430p-1f, -g));
+  const float p = __builtin_amdgcn_exp2f(fminf(hi, 127.5f));          // (never infinite: that times a lo below 0 would be NaN)
+  const float d = 1.f + fmaf(p, lo, p);
+  const float y = __builtin_amdgcn_rcpf(d);
+  return g * u * fmaf(fmaf(-y, d, 1.f), y, y);
 }
 
 template <int DT, bool GATE>
-__global__ __launch_bounds__(256) void proj_quant_kernel(const uint16_t* x, int64_t n_chunks, int row_chunks, int cols, uint8_t* codes, float* scales) {
-  // row_chunks: chunks of a row, up to the end of its last block
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = c / row_chunks;
-  const int at = (int)(c - row * row_chunks) * CHUNK;
-  const bool in = c < n_chunks && at < cols;
+__global__ __launch_bounds__(256) void proj_quant_kernel(const uint16_t* x, int rows, int row_chunks, int cols, uint8_t* codes, float* scales) {
+  // row_chunks: chunks of a row, up to the end of its last block.  Where a block begins is divided once, not for each thread.
+  const uint32_t first = blockIdx.x * 256u, first_row = first / (uint32_t)row_chunks;
+  uint32_t chunk = first - first_row * row_chunks + threadIdx.x, more = 0;
+  if (row_chunks >= 256) {
+    if (chunk >= (uint32_t)row_chunks) chunk -= row_chunks, more = 1;
+  } else {
+    more = chunk / (uint32_t)row_chunks;
+    chunk -= more * row_chunks;
+  }
+  const int64_t row = (int64_t)first_row + more;
+  const int at = (int)chunk * CHUNK;
+  const bool in = row < rows && at < cols;
   float v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = 0.f;
@@ -221,7 +225,7 @@ void launch_proj_quant(int dtype, const uint16_t* x, int rows, int cols, int til
   by_type(dtype, [&](auto dt) {
     if (tile == 1) {
       const int64_t n = (int64_t)rows * blocks * (QB / CHUNK);
-      hipLaunchKernelGGL((proj_quant_kernel<dt(), false>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, st, x, n, blocks * (QB / CHUNK), cols, codes, scales);
+      hipLaunchKernelGGL((proj_quant_kernel<dt(), false>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, st, x, rows, blocks * (QB / CHUNK), cols, codes, scales);
     } else {
       hipLaunchKernelGGL((proj_quant_tile_kernel<dt()>), dim3((uint32_t)blocks * blocks_of(rows)), dim3(256), 0, st, x, rows, cols, blocks, codes, scales);
     }
@@ -232,7 +236,7 @@ void launch_proj_gate(int dtype, const uint16_t* gu, int rows, int cols, uint8_t
   const int blocks = blocks_of(cols);
   const int64_t n = (int64_t)rows * blocks * (QB / CHUNK);
   by_type(dtype, [&](auto dt) {
-    hipLaunchKernelGGL((proj_quant_kernel<dt(), true>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, st, gu, n, blocks * (QB / CHUNK), cols, codes, scales);
+    hipLaunchKernelGGL((proj_quant_kernel<dt(), true>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, st, gu, rows, blocks * (QB / CHUNK), cols, codes, scales);
   });
 }
 
