@@ -38,11 +38,11 @@ __device__ __forceinline__ void store4(uint16_t* out, int64_t row, int c, int n,
 
 // 16 bytes of each lane into LDS behind each other, from `at` on; zeros where an offset is past the buffer's end
 __device__ __forceinline__ void load_lds(const int4v& buffer, uint32_t offset, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
 }
 // the same of 4 bytes
 __device__ __forceinline__ void load_lds4(const int4v& buffer, uint32_t offset, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
 __device__ __forceinline__ int4v buffer_of(const uint8_t* p, uint32_t bytes) {
@@ -488,7 +488,7 @@ Plan plan_of(int rows, int n, int cols) {
   for (int t = 0; t < (int)(sizeof(TILES) / sizeof(TILES[0])); ++t) {
     const int tn = ceil_div(n, TILES[t].tn), tm = ceil_div(rows, TILES[t].tm), slots = TILES[t].slots * CUS;
     for (int k = 1; k <= MAX_PARTS; ++k) {
-      if (k > 1 && blocks < k * LEAST_PART) break;
+      if (k > 1 && (blocks < k * LEAST_PART || (int64_t)tn * tm * (k - 1) >= slots)) break;
       const int per = ceil_div(blocks, k), splits = ceil_div(blocks, per);
       const int64_t work = (int64_t)tn * tm * splits, rounds = work / slots, rest = work % slots;
       float us = rounds * (per * (slots > CUS ? TILES[t].two : TILES[t].one) + TILES[t].results);

@@ -18,102 +18,151 @@ from .binding import FreeKVError, lib
 BLOCK = 128
 FEW_ROWS = 32                 # up to here a product needs no workspace
 CODES = torch.float8_e4m3fn
+F32, I32 = torch.float32, torch.int32
 _TYPES = {torch.float16: 0, torch.bfloat16: 1}
-_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
-def _refuse(t, what, dtype, shape, index):
-    where = f"cuda:{index}" if index >= 0 else "a GPU"
-    if not isinstance(t, torch.Tensor):
-        raise FreeKVError(f"{what}: a tensor is wanted, this is {type(t).__name__}")
-    raise FreeKVError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {where} is wanted, this is {t.dtype} {tuple(t.shape)} on {t.device}"
-                      + ("" if t.is_contiguous() else ", not contiguous"))
+# A call's kernel is a few microseconds of GPU time and so is the launch, so what is right is told in one expression, with few attribute
+# reads and no call in between (1 us less of 7 for a norm of one row); what is wrong is looked up afterwards.
+def _refuse(*wanted):
+    """Names the first of (name, tensor, types, shape, device) that is not as wanted."""
+    for what, t, types, shape, index in wanted:
+        if not isinstance(t, torch.Tensor):
+            raise FreeKVError(f"{what}: a tensor is wanted, this is {type(t).__name__}")
+        if t.dtype in types and tuple(t.shape) == tuple(shape) and t.is_contiguous() and t.get_device() == index and index >= 0:
+            continue
+        names = " or ".join(str(x).replace("torch.", "") for x in types)
+        where = f"cuda:{index}" if index >= 0 else "a GPU"
+        raise FreeKVError(f"{what}: a contiguous {names} tensor of shape {tuple(shape)} on {where} is wanted, this is {t.dtype} {tuple(t.shape)} on {t.device}"
+                          + ("" if t.is_contiguous() else ", not contiguous"))
+    raise FreeKVError("tensors that do not belong together")
 
 
-# (calls are a few microseconds of GPU time each, so what is right is told with few attribute reads)
-def _at(t, what, dtype, shape, index):
-    if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
-        return t.data_ptr()
-    _refuse(t, what, dtype, shape, index)
+def _shape(t, dims):
+    """A tensor's shape, or one that it cannot have."""
+    return tuple(t.shape) if isinstance(t, torch.Tensor) and t.dim() == dims else (-1,) * dims
 
 
-def _first(x, what, dims):
-    """Address, type code, type and device of the tensor that a call's shapes go by."""
-    if not isinstance(x, torch.Tensor) or x.dtype not in _TYPES or x.dim() != dims or not x.is_contiguous():
-        raise FreeKVError(f"{what}: a contiguous fp16 or bf16 tensor of {dims} dimensions on a GPU is wanted, this is "
-                          + (f"{x.dtype} {tuple(x.shape)} on {x.device}" if isinstance(x, torch.Tensor) else type(x).__name__))
-    index = x.get_device()
-    if index < 0:
-        raise FreeKVError(f"{what}: the projections are HIP kernels, this tensor is on {x.device}")
-    return x.data_ptr(), _TYPES[x.dtype], x.dtype, index
+def _device(t):
+    return t.get_device() if isinstance(t, torch.Tensor) else -1
 
 
-def _run(fn, what, index, *args, stream):
-    rc = fn(index, *args, _raw_stream(index) if stream is None else stream.cuda_stream)
-    if rc:
-        raise FreeKVError(f"{what}: {rc}: {lib().fkv_proj_last_error().decode()}")
+def _stream(stream, dev):
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _failed(rc, what):
+    raise FreeKVError(f"{what}: {rc}: {lib().fkv_proj_last_error().decode()}")
 
 
 def empty_quant(rows, cols, tile=1, device="cuda"):
     """Codes and scales for [rows, cols] values, not filled; tile: rows that share a scale, 1 or 128."""
     return (torch.empty((rows, cols), dtype=CODES, device=device),
-            torch.empty((-(-rows // tile), -(-cols // BLOCK)), dtype=torch.float32, device=device))
+            torch.empty((-(-rows // tile), -(-cols // BLOCK)), dtype=F32, device=device))
+
+
+def _eight_bits(what, x, dims, dev, codes, scales, rows, cols, tile=1):
+    """What _refuse() looks at for values and what they become."""
+    return ((what, x, _TYPES, _shape(x, dims), dev), ("codes", codes, (CODES,), (rows, cols), dev),
+            ("scales", scales, (F32,), (-(-rows // tile), -(-cols // BLOCK)), dev))
 
 
 def proj_quant(x, codes, scales, tile=1, stream=None):
     """x [rows, cols] into 8 bits; tile 1: activations, 128: weights."""
-    at, t, _, dev = _first(x, "x", 2)
     if tile != 1 and tile != BLOCK:
         raise FreeKVError("tile must be 1 or 128 rows")
-    rows, cols = x.shape
-    _run(lib().fkv_proj_quant, "fkv_proj_quant", dev, t, at, rows, cols, tile, _at(codes, "codes", CODES, (rows, cols), dev),
-         _at(scales, "scales", torch.float32, (-(-rows // tile), -(-cols // BLOCK)), dev), stream=stream)
+    rows, cols = shape = _shape(x, 2)
+    dev = _device(x)
+    try:
+        ok = (dev >= 0 and x.dtype in _TYPES and x.is_contiguous() and codes.dtype is CODES and codes.shape == shape and codes.is_contiguous()
+              and codes.get_device() == dev and scales.dtype is F32 and scales.shape == (-(-rows // tile), -(-cols // BLOCK)) and scales.is_contiguous()
+              and scales.get_device() == dev)
+    except AttributeError:       # (what is no tensor)
+        ok = False
+    if not ok:
+        _refuse(*_eight_bits("x", x, 2, dev, codes, scales, rows, cols, tile))
+    rc = lib().fkv_proj_quant(dev, _TYPES[x.dtype], x.data_ptr(), rows, cols, tile, codes.data_ptr(), scales.data_ptr(), _stream(stream, dev))
+    if rc:
+        _failed(rc, "fkv_proj_quant")
 
 
 def proj_norm(x, weight, codes=None, scales=None, add=None, res=None, out=None, eps=1e-5, stream=None):
     """The norm of x [rows, cols] (with `add`, of their sum, which is written to `res`, or into x where that is None) in 8 bits and / or, to
     `out`, in 16; weight [cols] or None."""
-    at, t, dtype, dev = _first(x, "x", 2)
-    rows, cols = x.shape
-    if add is None:
-        if res is not None:
-            raise FreeKVError("res: there is no sum without `add`")
-        a = r = None
-    else:
-        a, r = _at(add, "add", dtype, (rows, cols), dev), at if res is None else _at(res, "res", dtype, (rows, cols), dev)
+    rows, cols = shape = _shape(x, 2)
+    dev = _device(x)
+    if add is None and res is not None:
+        raise FreeKVError("res: there is no sum without `add`")
     if (codes is None) != (scales is None) or (codes is None and out is None):
         raise FreeKVError("codes and scales, or out, or all of them are wanted")
-    _run(lib().fkv_proj_norm, "fkv_proj_norm", dev, t, at, a, None if weight is None else _at(weight, "weight", dtype, (cols,), dev), rows, cols, eps, r,
-         None if codes is None else _at(codes, "codes", CODES, (rows, cols), dev),
-         None if scales is None else _at(scales, "scales", torch.float32, (rows, -(-cols // BLOCK)), dev),
-         None if out is None else _at(out, "out", dtype, (rows, cols), dev), stream=stream)
+    try:
+        ok = (dev >= 0 and (dtype := x.dtype) in _TYPES and x.is_contiguous()
+              and (weight is None or (weight.dtype is dtype and weight.shape == (cols,) and weight.is_contiguous() and weight.get_device() == dev))
+              and (codes is None or (codes.dtype is CODES and codes.shape == shape and codes.is_contiguous() and codes.get_device() == dev
+              and scales.dtype is F32 and scales.shape == (rows, -(-cols // BLOCK)) and scales.is_contiguous() and scales.get_device() == dev))
+              and (add is None or (add.dtype is dtype and add.shape == shape and add.is_contiguous() and add.get_device() == dev))
+              and (res is None or (res.dtype is dtype and res.shape == shape and res.is_contiguous() and res.get_device() == dev))
+              and (out is None or (out.dtype is dtype and out.shape == shape and out.is_contiguous() and out.get_device() == dev)))
+    except AttributeError:       # (what is no tensor)
+        ok = False
+    if not ok:
+        first, *eight = _eight_bits("x", x, 2, dev, codes, scales, rows, cols)
+        types = (x.dtype,) if isinstance(x, torch.Tensor) else ()
+        given = [(what, t, types, s, dev) for what, t, s in (("weight", weight, (cols,)), ("add", add, shape), ("res", res, shape), ("out", out, shape)) if t is not None]
+        _refuse(first, *(eight if codes is not None else ()), *given)
+    at = x.data_ptr()
+    rc = lib().fkv_proj_norm(dev, _TYPES[dtype], at, None if add is None else add.data_ptr(), None if weight is None else weight.data_ptr(), rows, cols, eps,
+                             None if add is None else at if res is None else res.data_ptr(), None if codes is None else codes.data_ptr(),
+                             None if codes is None else scales.data_ptr(), None if out is None else out.data_ptr(), _stream(stream, dev))
+    if rc:
+        _failed(rc, "fkv_proj_norm")
 
 
 def proj_gate(gu, codes, scales, stream=None):
     """silu(g) u of gu = [g, u], [rows, 2 cols], into 8 bits."""
-    at, t, _, dev = _first(gu, "gu", 2)
-    rows, cols = gu.shape
-    if cols % 2:
-        raise FreeKVError("gu: as many columns of the gate as of the other are wanted")
-    cols //= 2
-    _run(lib().fkv_proj_gate, "fkv_proj_gate", dev, t, at, rows, cols, _at(codes, "codes", CODES, (rows, cols), dev),
-         _at(scales, "scales", torch.float32, (rows, -(-cols // BLOCK)), dev), stream=stream)
+    rows, both = _shape(gu, 2)
+    cols, dev = both // 2, _device(gu)
+    try:
+        ok = (dev >= 0 and not both & 1 and gu.dtype in _TYPES and gu.is_contiguous() and codes.dtype is CODES and codes.shape == (rows, cols) and codes.is_contiguous()
+              and codes.get_device() == dev and scales.dtype is F32 and scales.shape == (rows, -(-cols // BLOCK)) and scales.is_contiguous() and scales.get_device() == dev)
+    except AttributeError:       # (what is no tensor)
+        ok = False
+    if not ok:
+        if both & 1 and both > 0:
+            raise FreeKVError("gu: as many columns of the gate as of the other are wanted")
+        _refuse(*_eight_bits("gu", gu, 2, dev, codes, scales, rows, cols))
+    rc = lib().fkv_proj_gate(dev, _TYPES[gu.dtype], gu.data_ptr(), rows, cols, codes.data_ptr(), scales.data_ptr(), _stream(stream, dev))
+    if rc:
+        _failed(rc, "fkv_proj_gate")
 
 
 def proj_rope(qkv, positions, freq, q, k, v, sections=None, stream=None):
     """qkv [rows, n_q + 2 n_kv, 128] apart into q, k, v, q and k turned by positions ([rows] or [axes, rows] int32) times freq ([64] fp32).
     sections: how many pairs of channels each axis has, one axis behind the other (64 in all), or each pair's axis (64 numbers); None: all the
     first axis'."""
-    at, t, dtype, dev = _first(qkv, "qkv", 3)
-    rows, heads, d = qkv.shape
-    n_q, n_kv = (x.shape[1] if isinstance(x, torch.Tensor) and x.dim() == 3 else 0 for x in (q, k))
-    if d != 128 or n_q + 2 * n_kv != heads:
-        raise FreeKVError(f"qkv: [rows, {n_q} + 2 x {n_kv}, 128] is wanted for this q and k, this is {tuple(qkv.shape)}")
-    axes = positions.shape[0] if positions.dim() == 2 else 1
-    _run(lib().fkv_proj_rope, "fkv_proj_rope", dev, t, at, rows, n_q, n_kv,
-         _at(positions, "positions", torch.int32, (axes, rows) if positions.dim() == 2 else (rows,), dev), axes, _axis_of(sections, axes),
-         _at(freq, "freq", torch.float32, (64,), dev), _at(q, "q", dtype, (rows, n_q, 128), dev), _at(k, "k", dtype, (rows, n_kv, 128), dev),
-         _at(v, "v", dtype, (rows, n_kv, 128), dev), stream=stream)
+    rows, heads, d = _shape(qkv, 3)
+    n_q, n_kv = (q.shape[1], k.shape[1]) if isinstance(q, torch.Tensor) and isinstance(k, torch.Tensor) and q.dim() == k.dim() == 3 else (0, 0)
+    dev = _device(qkv)
+    axes = positions.shape[0] if isinstance(positions, torch.Tensor) and positions.dim() == 2 else 0
+    try:
+        ok = (dev >= 0 and d == 128 and n_q + 2 * n_kv == heads and (dtype := qkv.dtype) in _TYPES and qkv.is_contiguous()
+              and q.dtype is dtype and q.shape == (rows, n_q, 128) and q.is_contiguous() and q.get_device() == dev
+              and k.dtype is dtype and k.shape == (kv := (rows, n_kv, 128)) and k.is_contiguous() and k.get_device() == dev
+              and isinstance(v, torch.Tensor) and v.dtype is dtype and v.shape == kv and v.is_contiguous() and v.get_device() == dev
+              and isinstance(positions, torch.Tensor) and positions.dtype is I32 and positions.shape == ((axes, rows) if axes else (rows,)) and positions.is_contiguous()
+              and positions.get_device() == dev
+              and isinstance(freq, torch.Tensor) and freq.dtype is F32 and freq.shape == (64,) and freq.is_contiguous() and freq.get_device() == dev)
+    except AttributeError:       # (what is no tensor)
+        ok = False
+    if not ok:
+        types = (qkv.dtype,) if isinstance(qkv, torch.Tensor) else ()
+        _refuse(("qkv", qkv, _TYPES, (rows, n_q + 2 * n_kv, 128), dev), ("q", q, types, (rows, n_q, 128), dev), ("k", k, types, (rows, n_kv, 128), dev),
+                ("v", v, types, (rows, n_kv, 128), dev), ("positions", positions, (I32,), (axes, rows) if axes else (rows,), dev), ("freq", freq, (F32,), (64,), dev))
+    axes = axes or 1
+    rc = lib().fkv_proj_rope(dev, _TYPES[dtype], qkv.data_ptr(), rows, n_q, n_kv, positions.data_ptr(), axes, None if sections is None else _axis_of(sections, axes),
+                             freq.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), _stream(stream, dev))
+    if rc:
+        _failed(rc, "fkv_proj_rope")
 
 
 _axes_known = {}
@@ -123,9 +172,9 @@ def _axis_of(sections, axes):
     """The C array of each pair's axis (arrays of the few sections that a program has are kept)."""
     if sections is None:
         return None
-    key = (tuple(sections), axes)
+    key = (*sections, axes)
     if key not in _axes_known:
-        given = key[0]
+        given = key[:-1]
         each = given if len(given) == 64 else tuple(a for a, n in enumerate(given) for _ in range(n))
         if len(each) != 64 or any(n < 0 for n in given) or (len(given) != 64 and len(given) > axes) or max(each) >= axes:
             raise FreeKVError(f"sections: parts of 64 pairs for {axes} axes, or 64 axes, are wanted, these are {given}")
@@ -137,17 +186,28 @@ def _axis_of(sections, axes):
 
 def proj_matmul(codes, scales, w, w_scales, out, stream=None):
     """out [rows, n] = x [rows, cols] w [n, cols]^T, both in 8 bits: scales [rows, ceil(cols / 128)], w_scales [ceil(n / 128), ceil(cols / 128)]."""
-    at, t, _, dev = _first(out, "out", 2)
-    rows, n = out.shape
-    cols = codes.shape[1] if codes.dim() == 2 else -1
-    blocks = -(-cols // BLOCK)
-    x, xs = _at(codes, "codes", CODES, (rows, cols), dev), _at(scales, "scales", torch.float32, (rows, blocks), dev)
-    ww, ws = _at(w, "w", CODES, (n, cols), dev), _at(w_scales, "w_scales", torch.float32, (-(-n // BLOCK), blocks), dev)
-    work, size = None, 0
+    rows, n = _shape(out, 2)
+    cols = _shape(codes, 2)[1]
+    dev, blocks = _device(out), -(-cols // BLOCK)
+    try:
+        ok = (dev >= 0 and out.dtype in _TYPES and out.is_contiguous()
+              and codes.dtype is CODES and codes.shape == (rows, cols) and codes.is_contiguous() and codes.get_device() == dev
+              and scales.dtype is F32 and scales.shape == (rows, blocks) and scales.is_contiguous() and scales.get_device() == dev
+              and w.dtype is CODES and w.shape == (n, cols) and w.is_contiguous() and w.get_device() == dev
+              and w_scales.dtype is F32 and w_scales.shape == (-(-n // BLOCK), blocks) and w_scales.is_contiguous() and w_scales.get_device() == dev)
+    except AttributeError:       # (what is no tensor)
+        ok = False
+    if not ok:
+        _refuse(("out", out, _TYPES, (rows, n), dev), ("codes", codes, (CODES,), (rows, cols), dev), ("scales", scales, (F32,), (rows, blocks), dev),
+                ("w", w, (CODES,), (n, cols), dev), ("w_scales", w_scales, (F32,), (-(-n // BLOCK), blocks), dev))
+    L, work, size = lib(), None, 0
     if rows > FEW_ROWS:
         need = C.c_size_t()
-        if lib().fkv_proj_workspace(rows, n, cols, C.byref(need)) == 0 and need.value:
+        if L.fkv_proj_workspace(rows, n, cols, C.byref(need)) == 0 and need.value:
             size = need.value
             with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):     # (the stream's own memory: it is free again behind this call's work)
                 work = torch.empty(size, dtype=torch.uint8, device=out.device)
-    _run(lib().fkv_proj_matmul, "fkv_proj_matmul", dev, t, x, xs, ww, ws, rows, n, cols, at, None if work is None else work.data_ptr(), size, stream=stream)
+    rc = L.fkv_proj_matmul(dev, _TYPES[out.dtype], codes.data_ptr(), scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(), rows, n, cols, out.data_ptr(),
+                           None if work is None else work.data_ptr(), size, _stream(stream, dev))
+    if rc:
+        _failed(rc, "fkv_proj_matmul")

@@ -131,3 +131,11 @@ def test_the_models_codes_are_the_types():
     for tile in (1, 128):
         codes, scales = M.quant(x, tile)
         assert ((M.values(codes, scales, tile) - x).abs() <= x.abs() * 2.0 ** -4 + M.spread(scales, 130, 200, tile) * 2.0 ** -10).all()
+
+
+def test_the_binding_refuses_what_is_no_tensor():
+    x = torch.zeros((4, 256), dtype=torch.bfloat16)
+    for call in (lambda: fkv.proj_quant(x, None, None), lambda: fkv.proj_norm(x, 1.0, None, None, out=3), lambda: fkv.proj_gate([1], None, None),
+                 lambda: fkv.proj_matmul(None, None, None, None, None), lambda: fkv.proj_matmul(x, x, x, x, "out"), lambda: fkv.proj_rope(x, 1, 2, 3, 4, 5)):
+        with pytest.raises(fkv.FreeKVError):
+            call()
