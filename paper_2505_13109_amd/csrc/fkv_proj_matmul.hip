@@ -61,11 +61,12 @@ constexpr uint32_t PAST = 0x80000000u;      // beyond any tile's bytes, also wit
 
 // ---- few rows: bound by the weights' bytes --------------------------------------------------------------------------
 // A block has 16 NT columns and all rows; its waves take the blocks of 128 in turn, each by itself, and their sums meet in LDS at the end.
-// Codes go straight into LDS, whole lines of memory at a time, PD blocks of each wave ahead: what is on its way takes no registers, and a wave waits
-// for nobody else.  16 bytes at place p of a row there are those at p ^ (row % 8) of the 128, so that the lanes of a wave, which want the same
-// columns of 16 rows, find them in different banks.
+// Codes go straight into LDS, whole lines of memory at a time, and are asked for as soon as those before are in registers: what is on its way takes
+// none, a wave waits for nobody else, and there is room for many of them on a compute unit.  (Two stages a wave are fewer waves: 16 rows x 28672 x 4096
+// 30.5 us, one 25.5.  Straight into registers, half a line of 16 rows at a time, 34.)  16 bytes at place p of a row there are those at
+// p ^ (row % 8) of the 128, so that the lanes of a wave, which want the same columns of 16 rows, find them in different banks.
 // Codes are turned into fp16, exactly: the fp16 instruction adds in fp32, where the 8-bit one cuts off what is below 2^-13 of the largest
-// product of eight, and memory leaves the time for it.
+// product of eight, and memory leaves the time for it (32 rows x 28672 x 4096 28.2 us, with 8-bit products 28.1).
 
 __device__ __forceinline__ void halves_of(const uint4& w, half8v* h) {       // 16 codes
   const uint32_t v[4] = {w.x, w.y, w.z, w.w};
@@ -79,24 +80,25 @@ __device__ __forceinline__ void halves_of(const uint4& w, half8v* h) {       // 
   }
 }
 
-constexpr int FEW_RUN = 128;                 // blocks of 128 whose scales are in LDS at a time
-
-template <int DT, int MT, int NT, int NW, int PD>
+// RUN: blocks of 128 whose scales are in LDS at a time
+template <int DT, int MT, int NT, int NW, int RUN>
 __global__ __launch_bounds__(NW * 64) void proj_few_kernel(ProjMatmul a) {
-  constexpr int STAGE = (NT + MT) * 16 * QB, LOADS = (NT + MT) * 2, RING = NW * PD * STAGE, SUMS = NW * MT * NT * 64 * 16;
-  __shared__ __attribute__((aligned(1024))) uint8_t s_ring[RING > SUMS ? RING : SUMS];
-  __shared__ float s_xs[(16 * MT * (FEW_RUN + 1) + 63) / 64 * 64], s_ws[FEW_RUN];
+  constexpr int STAGE = (NT + MT) * 16 * QB, LOADS = (NT + MT) * 2, RING = NW * STAGE, SUMS = NW * MT * NT * 64 * 16;
+  static_assert(RUN % 64 == 0, "");
+  __shared__ __attribute__((aligned(1024))) uint8_t s_stage[RING > SUMS ? RING : SUMS];
+  __shared__ float s_xs[(16 * MT * (RUN + 1) + 63) / 64 * 64], s_ws[RUN];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
   const int blocks = blocks_of(a.cols), c0 = blockIdx.x * 16 * NT;
   const int4v wbuf = buffer_of(a.w + (int64_t)c0 * a.cols, (uint32_t)min(16 * NT, a.n - c0) * (uint32_t)a.cols), xbuf = buffer_of(a.x, (uint32_t)a.rows * (uint32_t)a.cols);
   const int4v wsbuf = buffer_of((const uint8_t*)(a.ws + (int64_t)(c0 / QB) * blocks), (uint32_t)blocks * 4), xsbuf = buffer_of((const uint8_t*)a.xs, (uint32_t)(a.rows * blocks) * 4);
-  const uint32_t ring = lds_of(s_ring) + wave * (PD * STAGE), chunk = ((lane & 7) ^ (lane >> 3)) * 16, from = (uint32_t)(lane >> 3) * (uint32_t)a.cols + chunk;
-  auto bring = [&](int b, int slot) {
+  const uint32_t chunk = ((lane & 7) ^ (lane >> 3)) * 16, from = (uint32_t)(lane >> 3) * (uint32_t)a.cols + chunk;
+  const uint8_t* stage = s_stage + wave * STAGE;
+  auto bring = [&](int b) {
     const uint32_t off = b * QB + (int)chunk < a.cols ? from + (uint32_t)(b * QB) : PAST;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const bool is_w = i < 2 * NT;
-      load_lds(is_w ? wbuf : xbuf, off + (uint32_t)(i - (is_w ? 0 : 2 * NT)) * 8 * (uint32_t)a.cols, ring + slot * STAGE + i * 1024);
+      load_lds(is_w ? wbuf : xbuf, off + (uint32_t)(i - (is_w ? 0 : 2 * NT)) * 8 * (uint32_t)a.cols, lds_of(s_stage) + wave * STAGE + i * 1024);
     }
   };
   float4v acc[MT][NT];
@@ -105,26 +107,24 @@ __global__ __launch_bounds__(NW * 64) void proj_few_kernel(ProjMatmul a) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
   const int lo = t * QB + ((g ^ (t & 7)) * 16), hi = lo ^ 64;
-  for (int run = 0; run < blocks; run += FEW_RUN) {
-    const int end = min(blocks, run + FEW_RUN), held = end - run, pitch = held | 1;        // (rows of scales begin in different banks)
+  for (int run = 0; run < blocks; run += RUN) {
+    const int end = min(blocks, run + RUN), held = end - run, pitch = held | 1;            // (rows of scales begin in different banks)
     if (run) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");               // everybody is done with the scales before
     for (int e = wave * 64; e < a.rows * pitch; e += NW * 64) {
       const int i = e + lane, r = i / pitch, b = i - r * pitch;
       load_lds4(xsbuf, r < a.rows && b < held ? (uint32_t)(r * blocks + run + b) * 4u : PAST, lds_of(s_xs) + e * 4);
     }
     for (int e = wave * 64; e < held; e += NW * 64) load_lds4(wsbuf, (uint32_t)(run + e + lane) * 4u, lds_of(s_ws) + e * 4);
-    int b = run + wave, asked = b;
-#pragma unroll
-    for (int i = 0; i < PD; ++i)
-      if (asked < end) bring(asked, i), asked += NW;
-    // loads end in order: the scales are there when no more than the stages' are on their way
-    if (b + (PD - 1) * NW < end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PD * LOADS) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    int b = run + wave;
+    if (b < end) {
+      bring(b);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");                         // (loads end in order: the scales are there)
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
     asm volatile("s_barrier" ::: "memory");
-    for (int slot = 0; b < end; b += NW, slot = slot + 1 < PD ? slot + 1 : 0) {
-      if (b + (PD - 1) * NW < end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((PD - 1) * LOADS) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      const uint8_t* stage = s_ring + wave * (PD * STAGE) + slot * STAGE;
+    for (; b < end; b += NW) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       uint4 w[NT][2], x[MT][2];
       float s[MT];
 #pragma unroll
@@ -134,11 +134,9 @@ __global__ __launch_bounds__(NW * 64) void proj_few_kernel(ProjMatmul a) {
       const float ws = s_ws[b - run];
 #pragma unroll
       for (int i = 0; i < MT; ++i) s[i] = s_xs[(16 * i + t) * pitch + b - run] * ws;
-      if (asked < end) {
-        // the operands are in registers, so their place is free
+      if (b + NW < end) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        bring(asked, slot);
-        asked += NW;
+        bring(b + NW);
       }
       half8v wh[NT][4];
 #pragma unroll
@@ -159,7 +157,7 @@ __global__ __launch_bounds__(NW * 64) void proj_few_kernel(ProjMatmul a) {
     }
   }
   __syncthreads();
-  float4v* sums = reinterpret_cast<float4v*>(s_ring);              // [wave][tile][lane]
+  float4v* sums = reinterpret_cast<float4v*>(s_stage);              // [wave][tile][lane]
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -470,18 +468,19 @@ constexpr struct { int tn, tm, slots; float one, two, results; } TILES[] = {
 constexpr float READ_RATE = 4.5e6f, JOIN = 3.f, JOIN_RATE = 7.5e6f;       // bytes a us of weights, us of a join's launch, bytes a us of parts
 constexpr int MAX_PARTS = 16, LEAST_PART = 4;
 
-// Up to 32 rows the weights' bytes are what counts, beyond it is tiles.  32 rows x 28672 x 4096: 34 us, as tiles 33; 32 x 6144 x 4096: 9.1 and 12.2;
-// 48 rows as tiles 34 and 13.4, three tiles of 16 rows at a time 57 and 18.
-// Few rows: two tiles of 16 columns to a block, as its waves read all activations (16 rows x 28672 x 4096 26.3 us, one 28.2), but where that
-// leaves compute units without a block and each wave much to read (16 rows x 4096 x 14336: 14.7 us, one tile and eight waves 12.2).
+// Few rows are bound by the weights' bytes.  A block's waves read all activations, so two tiles of 16 columns go to a block, four of
+// more than 16 rows where there are blocks for all compute units all the same (32 rows x 28672 x 4096 27.6 us, two 29.3; 32 x 6144 x 4096 12.9 and
+// 9.8), but one, with more waves, where few columns are long (16 rows x 4096 x 14336 14.8 us, two 18.3).  Beyond 32 rows that is faster than
+// tiles while a block a compute unit has all columns and they are not long (48 x 6144 x 4096 10.9 us, tiles 15.2; 48 x 4096 x 14336 26 and 22;
+// 48 x 28672 x 4096 37.5 and 35).
 Plan plan_of(int rows, int n, int cols) {
   Plan p{};
   const int blocks = blocks_of(cols);
-  if (rows <= 32) {
+  if (rows <= 32 || (rows <= 64 && ceil_div(n, 32) <= CUS && blocks <= 64)) {
     p.few = true;
-    const bool narrow = ceil_div(n, 32) < CUS && blocks > 48;
-    p.nt = narrow ? 1 : 2;
-    p.nw = narrow ? 8 : 4;
+    const bool narrow = rows <= 32 && ceil_div(n, 32) < CUS && blocks > 48, wide = rows > 16 && rows <= 32 && ceil_div(n, 64) > CUS;
+    p.nt = narrow ? 1 : wide ? 4 : 2;
+    p.nw = narrow && rows <= 16 ? 16 : wide ? 4 : 8;
     return p;
   }
   float best = 0.f;
@@ -517,10 +516,18 @@ void launch_proj_matmul(int dtype, const ProjMatmul& a, hipStream_t st) {
   auto go = [&](auto dt) {
     if (p.few) {
       const dim3 grid((uint32_t)ceil_div(a.n, 16 * p.nt)), block((uint32_t)p.nw * 64);
-      if (p.nt == 1 && a.rows <= 16) hipLaunchKernelGGL((proj_few_kernel<dt(), 1, 1, 8, 2>), grid, block, 0, st, a);
-      else if (p.nt == 1) hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 1, 8, 2>), grid, block, 0, st, a);
-      else if (a.rows <= 16) hipLaunchKernelGGL((proj_few_kernel<dt(), 1, 2, 4, 2>), grid, block, 0, st, a);
-      else hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 2, 4, 2>), grid, block, 0, st, a);
+      if (a.rows <= 16) {
+        if (p.nt == 1) hipLaunchKernelGGL((proj_few_kernel<dt(), 1, 1, 16, 128>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((proj_few_kernel<dt(), 1, 2, 8, 64>), grid, block, 0, st, a);
+      } else if (a.rows <= 32) {
+        if (p.nt == 1) hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 1, 8, 128>), grid, block, 0, st, a);
+        else if (p.nt == 2) hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 2, 8, 64>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 4, 4, 64>), grid, block, 0, st, a);
+      } else if (a.rows <= 48) {
+        hipLaunchKernelGGL((proj_few_kernel<dt(), 3, 2, 8, 64>), grid, block, 0, st, a);
+      } else {
+        hipLaunchKernelGGL((proj_few_kernel<dt(), 4, 2, 8, 64>), grid, block, 0, st, a);
+      }
       return;
     }
     const dim3 grid((uint32_t)std::min((int64_t)p.g.tn * p.g.tm * p.g.splits, (int64_t)TILES[p.tile].slots * CUS));
