@@ -181,7 +181,8 @@ __global__ __launch_bounds__(NW * 64) void proj_few_kernel(ProjMatmul a) {
 // A block works on tiles of TN columns and TM rows, one behind the other, its waves on WN x WM parts of them.  The codes of a block of 128 columns
 // go straight into LDS, ST - 1 of them ahead of the one that is multiplied (of the next tile, where this one's have been asked for), so that
 // neither the operands nor the results of a tile are waited for; 16 bytes at place p of a row there are those at p ^ (row % 8) of the 128, so
-// that the lanes of a wave, which want the same columns of 16 rows, find them in different banks.
+// that the lanes of a wave, which want the same columns of 16 rows, find them in different banks.  A SIMD has two waves, so that one multiplies
+// where the other meets the rest or adds (203 rows x 4096 x 11056 in tiles of 128 with one wave a SIMD 30 us, with two 27).
 
 struct Tiles {
   int tn, tm;                 // columns' and rows' tiles
@@ -338,6 +339,7 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void proj_many_kernel(ProjMatmul a
       const bool last = nth == SB - 1 || b + 1 == here.b1;
 #pragma unroll
       for (int i = 0; i < AN - 2; ++i) {
+        if (i == 2) begin();
         if (i == 1)
 #pragma unroll
           for (int j = 0; j < AM; ++j) s[j] = s_next[j] * ws_next;
@@ -353,12 +355,12 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void proj_many_kernel(ProjMatmul a
             for (int k = at * N / PLACES; k < (at + 1) * N / PLACES; ++k) bring(NA + k);
         }
       }
+      if (AN - 2 <= 2) begin();
       stage = stage + 1 < ST ? stage + 1 : 0;
       // (the next run's scales were asked for at the end of the one before this: too few loads ago where this one is short)
       if (ST > 2 && last && nth < ST - 3) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((ST - 2) * LOADS) : "memory");
       if (last) scales(which);
-      begin();
       nth = last ? 0 : nth + 1;
       which ^= last;
       wv[0] = operand(stage, row_w(0));
@@ -461,11 +463,11 @@ struct Plan {
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // The tiles that many rows are cut into, and what they cost, in us: a block of 128 columns where a compute unit has one of them and where it has
-// two, and a tile's results.  From products of 48 to 1024 rows (n x cols of 4096 x 11056 and x 14336, 6144 and 28672 x 4096, 8192 x 8192,
-// 1 to 16 parts), whose times these give within 8 %.
+// two, and a tile's results.  From products of 48 to 2048 rows (n x cols of 4096 x 11056 and x 14336, 6144 and 28672 x 4096, 8192 x 8192,
+// 1 to 16 parts), whose times these give within 8 %; what they choose took at most 10 % longer than the best of all, 1 or 2 % as a rule.
 constexpr struct { int tn, tm, slots; float one, two, results; } TILES[] = {
-    {64, 64, 2, 0.40f, 0.58f, 0.f}, {128, 128, 1, 0.76f, 0.76f, 2.f}, {128, 128, 2, 1.38f, 1.45f, 1.f}, {256, 256, 1, 2.0f, 2.0f, 0.f}};
-constexpr float READ_RATE = 4.5e6f, JOIN = 3.f, JOIN_RATE = 7.5e6f;       // bytes a us of weights, us of a join's launch, bytes a us of parts
+    {64, 64, 2, 0.40f, 0.58f, 0.f}, {128, 128, 1, 0.72f, 0.72f, 2.f}, {128, 128, 2, 1.28f, 1.35f, 1.f}, {256, 256, 1, 2.0f, 2.0f, 0.f}};
+constexpr float READ_RATE = 4.5e6f, JOIN = 3.f, JOIN_RATE = 5.5e6f;       // bytes a us of weights, us of a join's launch, bytes a us of parts
 constexpr int MAX_PARTS = 16, LEAST_PART = 4;
 
 // Few rows are bound by the weights' bytes.  A block's waves read all activations, so two tiles of 16 columns go to a block, four of
@@ -496,10 +498,6 @@ Plan plan_of(int rows, int n, int cols) {
       if (splits > 1) us += JOIN + 8.f * splits * rows * n / JOIN_RATE;
       if (best == 0.f || us < best) best = us, p.tile = t, p.g = {tn, tm, splits, per};
     }
-  }
-  if (const int t = knob("FKV_TILE", -1); t >= 0) {
-    const int k = knob("FKV_SPLITS", 1), per = ceil_div(blocks, k);
-    p.tile = t, p.g = {ceil_div(n, TILES[t].tn), ceil_div(rows, TILES[t].tm), ceil_div(blocks, per), per};
   }
   return p;
 }
@@ -533,7 +531,7 @@ void launch_proj_matmul(int dtype, const ProjMatmul& a, hipStream_t st) {
     const dim3 grid((uint32_t)std::min((int64_t)p.g.tn * p.g.tm * p.g.splits, (int64_t)TILES[p.tile].slots * CUS));
     auto many = [&](auto split) {
       if (p.tile == 0) hipLaunchKernelGGL((proj_many_kernel<dt(), 64, 64, 1, 4, 4, 16, split()>), grid, dim3(256), 0, st, a, p.g);
-      else if (p.tile == 1) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, 4, 16, split()>), grid, dim3(256), 0, st, a, p.g);
+      else if (p.tile == 1) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 4, 4, 16, split()>), grid, dim3(512), 0, st, a, p.g);
       else if (p.tile == 2) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, 2, 8, split()>), grid, dim3(256), 0, st, a, p.g);
       else hipLaunchKernelGGL((proj_many_kernel<dt(), 256, 256, 2, 4, 2, 8, split()>), grid, dim3(512), 0, st, a, p.g);
     };
