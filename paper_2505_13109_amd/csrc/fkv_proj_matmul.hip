@@ -315,6 +315,7 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void proj_many_kernel(ProjMatmul a
     for (int j = 0; j < AM; ++j) s_next[j] = s_xs[which][wm * CM + 16 * j + t][nth];
   };
   next_scales();
+  __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt(0): or the loop would begin with a wait for what may be on its way here, every time
   for (int id = blockIdx.x; id < total; id += gridDim.x) {
     float4v acc[AN][AM], p[AM];
     float s[AM], s_before[AM];
@@ -409,7 +410,9 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void proj_many_kernel(ProjMatmul a
         }
       }
     } else {
-      // through LDS, a wave by itself: 16 rows of OC columns, whole lines of the result
+      static_assert(OS == 4, "");
+      // through LDS, a wave by itself: 16 rows of OC columns, whole lines of the result; four rows are all banks once, so a part's place changes
+      // from one four to the next
       uint16_t* tile = s_out[wave];
 #pragma unroll
       for (int j = 0; j < AM; ++j)
@@ -418,14 +421,14 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void proj_many_kernel(ProjMatmul a
 #pragma unroll
           for (int i = 0; i < OC / 16; ++i) {
             const float4v& v = acc[o / 16 + i][j];
-            *reinterpret_cast<uint2*>(tile + out_t * OC + ((2 * i + (out_gr >> 1)) ^ (out_t & (OS - 1))) * 8 + (out_gr & 1) * 4) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+            *reinterpret_cast<uint2*>(tile + out_t * OC + ((2 * i + (out_gr >> 1)) ^ (out_t / OS)) * 8 + (out_gr & 1) * 4) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
           }
           __builtin_amdgcn_wave_barrier();
 #pragma unroll
           for (int k = 0; k < 16 * OS / 64; ++k) {
             const int r = k * (64 / OS) + out_lane / OS, c = cw + o + out_lane % OS * 8;
             const int64_t row = here.r0 + wm * CM + 16 * j + r;
-            const uint4 v = *reinterpret_cast<const uint4*>(tile + r * OC + ((out_lane % OS) ^ (r & (OS - 1))) * 8);
+            const uint4 v = *reinterpret_cast<const uint4*>(tile + r * OC + ((out_lane % OS) ^ (r / OS)) * 8);
             if (row < a.rows && c < a.n) *reinterpret_cast<uint4*>(a.out + row * a.n + c) = v;
           }
           __builtin_amdgcn_wave_barrier();

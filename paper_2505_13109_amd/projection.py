@@ -173,15 +173,16 @@ def _axis_of(sections, axes):
     if sections is None:
         return None
     key = (*sections, axes)
-    if key not in _axes_known:
+    known = _axes_known.get(key)
+    if known is None:
         given = key[:-1]
         each = given if len(given) == 64 else tuple(a for a, n in enumerate(given) for _ in range(n))
         if len(each) != 64 or any(n < 0 for n in given) or (len(given) != 64 and len(given) > axes) or max(each) >= axes:
             raise FreeKVError(f"sections: parts of 64 pairs for {axes} axes, or 64 axes, are wanted, these are {given}")
         if len(_axes_known) >= 64:
             _axes_known.clear()
-        _axes_known[key] = (C.c_int32 * 64)(*each)
-    return _axes_known[key]
+        known = _axes_known[key] = (C.c_int32 * 64)(*each)
+    return known
 
 
 def proj_matmul(codes, scales, w, w_scales, out, stream=None):

@@ -29,12 +29,12 @@ def exact(x, xs, w, ws):
     return spread(xs, x, 1) @ spread(ws, w, 128).T
 
 
-FEW = [(1, 33, 33040), (7, 600, 131072), (20, 4099, 20000), (32, 50, 16400), (17, 20000, 272), (9, 9001, 16)]
+FEW = [(1, 33, 33040), (7, 600, 131072), (20, 4099, 20000), (32, 50, 16400), (17, 20000, 272), (9, 9001, 16), (63, 4099, 2064), (49, 1, 8192)]
 # rows, n, cols: a tile of 64, 128 (four stages, two) and 256 squared; whole and in parts; one to a block and more; runs of scales of one block to many
 MANY = [(33, 1, 16), (130, 16848, 2416), (137, 11029, 400), (198, 10556, 16), (39, 6763, 2080), (414, 18, 464), (232, 116, 128), (36, 16633, 7936), (40, 2958, 10384),
         (254, 1, 2560), (50, 100, 131072), (74, 16811, 2320), (75, 17604, 1216), (66, 5379, 10800), (69, 6135, 3840), (799, 16609, 2064), (1070, 13195, 400),
         (869, 16468, 160), (210, 17959, 2144), (271, 16457, 416), (1361, 4433, 144), (69, 13105, 8640), (65, 5508, 8352), (1560, 10161, 2064), (1169, 14538, 416),
-        (2389, 6710, 16), (386, 17590, 2192), (775, 9847, 416), (714, 8648, 16), (140, 16858, 6320), (130, 6298, 5104)]
+        (2389, 6710, 16), (386, 17590, 2192), (775, 9847, 416), (714, 8648, 16), (140, 16858, 6320), (130, 6298, 5104), (2630, 6370, 3472)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])

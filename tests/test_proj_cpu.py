@@ -119,6 +119,17 @@ def test_sections():
             _axis_of(bad, axes)
 
 
+def test_more_sections_than_are_kept_from_several_threads():
+    from concurrent.futures import ThreadPoolExecutor
+    from paper_2505_13109_amd.projection import _axis_of
+
+    def ask(first):
+        return all(list(_axis_of((n, 64 - n), 2)) == [0] * n + [1] * (64 - n) for i in range(30) for n in range(first, 65))
+
+    with ThreadPoolExecutor(8) as pool:
+        assert all(pool.map(ask, range(8)))
+
+
 def test_the_models_codes_are_the_types():
     """All e4m3 numbers, and what lies between them, against the type's own conversion (which rounds to even)."""
     every = torch.arange(0, 127, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
