@@ -1,4 +1,5 @@
-// Values into 8 bits: as they are, behind the norm, behind the gated activation.  Bound by memory: every value is read once.
+// Values into 8 bits: as they are, behind the norm, behind the gated activation.  Bound by memory: every value is read once, from 5.0 to 5.4 TB/s for large calls
+// (a copy reaches 5.1); a call of a few rows is a launch and one round trip to memory, 2 to 3 us.
 // A thread has eight adjacent columns (16 bytes of T), so a block of 128 is a row of 16 lanes and its largest value four steps away.
 #include "fkv_proj_dev.h"
 
@@ -16,7 +17,8 @@ __device__ __forceinline__ uint4 load16(const uint16_t* p) { return *reinterpret
 
 // g / (1 + exp(-g)) u.  exp(-g) = 2^hi (1 + lo) with hi ln 2 + lo = -g to 48 bits; the reciprocal is the nearest but for its last
 // place, and the product g u is exact for bf16 and has 22 of 24 bits for fp16: about a rounding each for exp, sum, reciprocal and result.
-// (With exp(-|g|), a quotient and the sum's own rounding, nine more of 40 instructions a value: 4096 x 14336 73 us.)
+// Some 40 instructions a value with its code, which take nearly as long as memory: 4096 x 14336 56 to 62 us, 4.8 to 5.3 TB/s; 33 x 12544 2.5 us.
+// (With exp(-|g|), a quotient and the sum's own rounding, nine more: 73 us.)
 __device__ __forceinline__ float gated(float g, float u) {
   const float hi = g * -0x1.715476p+0f, lo = fmaf(hi, 0x1.05c610p-29f, fmaf(hi, -0x1.62e430p-1f, -g));
   const float p = __builtin_amdgcn_exp2f(fminf(hi, 127.5f));          // (never infinite: that times a lo below 0 would be NaN)
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(256) void proj_quant_kernel(const uint16_t* x, int 
   }
 }
 
-// 128 rows a scale: a block of 256 threads has one of weights, in registers
+// 128 rows a scale: a block of 256 threads has one of weights, in registers, so that they are read once (28672 x 4096 65 us, 5.4 TB/s)
 template <int DT>
 __global__ __launch_bounds__(256) void proj_quant_tile_kernel(const uint16_t* x, int rows, int cols, int blocks, uint8_t* codes, float* scales) {
   __shared__ uint32_t s_top[4];
@@ -106,6 +108,7 @@ __global__ __launch_bounds__(256) void proj_quant_tile_kernel(const uint16_t* x,
 // Codes are those of s weight, which the inputs alone decide; the row's factor goes into the scales.  So a chunk's codes are written
 // before the row's sum is known, and only a scale waits for it.  Squares are summed in fp64: they pass fp32's range where bf16 values do
 // not.  CH chunks a thread are in registers (of a row that is longer, so many at a time: its products are made again for `out`).
+// Bound by memory: 4096 x 8192 with the residual 45 us, 5.2 TB/s, of which the fp64 of the sum (an instruction a value) hides behind the loads.
 template <int DT, int NT, int CH, bool ADD, bool OUT>
 __global__ __launch_bounds__(NT) void proj_norm_kernel(ProjNorm a) {
   __shared__ double s_sum[NT / 64];
@@ -240,11 +243,21 @@ void launch_proj_gate(int dtype, const uint16_t* gu, int rows, int cols, uint8_t
   });
 }
 
+// A block's threads are the fewest that hold a row, up to 512 with two chunks each: 8192 rows of 1024 columns 12.5 us with 128 threads, 23.8 with 512,
+// 32.6 with 512 that have two; 8192 x 2048 24.3 with 256, 28.8 and 35.4; 4096 x 8192 45 with 512 x 2, 46 with 1024, 49 with 256.  Rows that
+// are longer are gone through twice, 1024 threads at a time (64 x 32768 9.3 us, 512 x 2 10.5).  One row takes 2.4 to 3.6 us up to 8192.
 void launch_proj_norm(int dtype, const ProjNorm& a, hipStream_t st) {
   by_type(dtype, [&](auto dt) {
     by_flag(a.add != nullptr, [&](auto add) {
       by_flag(a.out != nullptr, [&](auto out) {
-        hipLaunchKernelGGL((proj_norm_kernel<dt(), 512, 2, add(), out()>), dim3((uint32_t)a.rows), dim3(512), 0, st, a);
+        auto go = [&](auto nt, auto ch) {
+          hipLaunchKernelGGL((proj_norm_kernel<dt(), nt(), ch(), add(), out()>), dim3((uint32_t)a.rows), dim3(nt()), 0, st, a);
+        };
+        if (a.cols <= 1024) go(std::integral_constant<int, 128>(), std::integral_constant<int, 1>());
+        else if (a.cols <= 2048) go(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
+        else if (a.cols <= 4096) go(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
+        else if (a.cols <= 8192) go(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
+        else go(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
       });
     });
   });

@@ -134,7 +134,7 @@ def test_blocks_with_nan_or_infinities_stand_for_nan_alone(tile):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("add,weight,quant,out", [(True, True, True, False), (True, False, True, True), (False, True, True, True), (False, False, False, True), (True, True, False, True)])
-@pytest.mark.parametrize("rows,cols", [(1, 16), (3, 3584), (2, 4112), (65, 8192), (700, 256), (2, 32784), (3, 131072)])
+@pytest.mark.parametrize("rows,cols", [(1, 16), (33, 1024), (9, 1040), (5, 2048), (3, 2064), (3, 3584), (2, 4112), (65, 8192), (7, 8208), (700, 256), (2, 32784), (3, 131072)])
 def test_norm_is_the_definition(rows, cols, add, weight, quant, out, dtype):
     x = randn(rows, cols, seed=1, dtype=dtype)
     a = randn(rows, cols, seed=2, dtype=dtype, outliers=False) if add else None
@@ -268,7 +268,7 @@ def rope_of(rows, n_q, n_kv, positions, dtype, sections=None, axis_of=None, seed
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,n_q,n_kv", [(1, 1, 1), (1, 32, 8), (5, 28, 4), (67, 7, 1), (1100, 12, 3), (2, 300, 300)])
+@pytest.mark.parametrize("rows,n_q,n_kv", [(1, 1, 1), (6, 4, 1), (1, 32, 8), (5, 28, 4), (67, 7, 1), (1100, 12, 3), (9, 12, 3), (2, 300, 300)])
 def test_rope_of_one_axis(rows, n_q, n_kv, dtype):
     positions = torch.randint(0, 40000, (rows,), generator=gen(rows), dtype=torch.int32)
     rope_of(rows, n_q, n_kv, positions, dtype)
