@@ -39,8 +39,8 @@ int fkv_proj_quant(int32_t device, int32_t dtype, const void* x_dev, int32_t row
 int fkv_proj_norm(int32_t device, int32_t dtype, const void* x_dev, const void* add_dev, const void* weight_dev, int32_t rows, int32_t cols, float eps,
                   void* res_dev, void* codes_dev, float* scales_dev, void* out_dev, void* stream);
 
-/* gu dev [rows, 2 cols] of T, the gate's columns before the others': g / (1 + exp(-g)) u in fp32, into 8 bits.  Sigmoids below 2^-126 count as no more
- * than that; g u beyond fp32's largest is infinite. */
+/* gu dev [rows, 2 cols] of T, the gate's columns before the others': g / (1 + exp(-g)) u in fp32, into 8 bits.  Sigmoids below 2^-126 count as 0,
+ * whatever g's size; g u beyond fp32's largest is infinite. */
 int fkv_proj_gate(int32_t device, int32_t dtype, const void* gu_dev, int32_t rows, int32_t cols, void* codes_dev, float* scales_dev, void* stream);
 
 /* q, k and v out of the packed product, q and k turned by their rotary positions:
