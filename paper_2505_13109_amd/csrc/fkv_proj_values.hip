@@ -15,24 +15,34 @@ __device__ __forceinline__ uint4 load16(const uint16_t* p) { return *reinterpret
 
 // ---- plain values, and the gate: a thread one chunk of a row -------------------------------------------------
 
-// g / (1 + exp(-g)) u.  exp(-g) = 2^hi (1 + lo) with hi ln 2 + lo = -g to 48 bits; the reciprocal is the nearest but for its last
-// place, and the product g u is exact for bf16 and has 22 of 24 bits for fp16: about a rounding each for exp, sum, reciprocal and result.
-// Only between the ends e does the exponential depend on g: above 128 it is nothing to 1; at -88.37 it is 2^127.49, whose reciprocal, like all
-// below 2^-126, is 0.  With g itself hi would be as coarse as fp32 is there, and lo, what hi leaves, no small number any more.
-// Some 40 instructions a value with its code, which take nearly as long as memory: 4096 x 14336 56 to 62 us, 4.8 to 5.3 TB/s; 33 x 12544 2.5 us.
-// (With exp(-|g|), a quotient and the sum's own rounding, nine more: 73 us.)
+// g / (1 + exp(-g)) u, g u being exact.  exp(-g) = 2^hi exp(lo) with hi near -g log2(e) and lo, which is hi ln 2 + g, so small that 1 + lo will do:
+// for bf16 hi is an exact product with 15 bits of log2(e) (lo^2 / 2 is 2^-24 at |g| = 70 and below 2^-28 to 17), for fp16 it is the nearest and lo
+// taken with ln 2 in two parts.  The quotient's remainder, g u - t (1 + q), is taken from q = exp(-g) itself and not from the rounded sum, exactly as long as q
+// is at most 1: so the result is rounded once, and what q is off by counts as q / (1 + q) of it.
+// Only between the ends e does the exponential depend on g: above 128 it is nothing to 1; at -88.5 it is 2^127.7, whose reciprocal, like all
+// below 2^-126, is 0.  With g itself hi would be as coarse as fp32 is there, and lo no small number any more.
+// Some 40 instructions a value with its code, which take nearly as long as memory: 4096 x 14336 58 to 62 us, 4.8 to 5.1 TB/s; 33 x 12544 2.5 us.
+// (The remainder from the sum and what that was rounded by, two more: 4 to 6 % longer, and a mean error of 0.41 x 2^-24 instead of 0.48.)
+template <int DT>
 __device__ __forceinline__ float gated(float g, float u) {
-  const float e = __builtin_amdgcn_fmed3f(g, -88.37f, 128.f);
-  const float hi = e * -0x1.715476p+0f, lo = fmaf(hi, 0x1.05c610p-29f, fmaf(hi, -0x1.62e430p-1f, -e));
-  const float p = __builtin_amdgcn_exp2f(hi);
-  const float d = 1.f + fmaf(p, lo, p);
-  const float y = __builtin_amdgcn_rcpf(d);
-  return g * u * fmaf(fmaf(-y, d, 1.f), y, y);
+  const float e = __builtin_amdgcn_fmed3f(g, -88.5f, 128.f);
+  float hi, lo;
+  if (DT == 1) {
+    hi = e * -0x1.7154p+0f;
+    lo = e * -0x1.480fb6p-18f;
+  } else {
+    hi = e * -0x1.715476p+0f;
+    lo = fmaf(hi, 0x1.05c610p-29f, fmaf(hi, -0x1.62e430p-1f, -e));
+  }
+  const float p = __builtin_amdgcn_exp2f(hi), q = fmaf(p, lo, p);
+  const float y = __builtin_amdgcn_rcpf(1.f + q), w = g * u, t = w * y;
+  return fmaf(fmaf(-t, q, w - t), y, t);
 }
 
 template <int DT, bool GATE>
 __global__ __launch_bounds__(256) void proj_quant_kernel(const uint16_t* x, int rows, int row_chunks, int cols, uint8_t* codes, float* scales) {
-  // row_chunks: chunks of a row, up to the end of its last block.  Where a block begins is divided once, not for each thread.
+  // row_chunks: chunks of a row, up to the end of its last block.  Where a block begins is divided once, not for each thread, and what
+  // lies before it in memory is the same for all: a thread's own offsets, of at most 255 rows of 2048 columns or one longer one, have 32 bits.
   const uint32_t first = blockIdx.x * 256u, first_row = first / (uint32_t)row_chunks;
   uint32_t chunk = first - first_row * row_chunks + threadIdx.x, more = 0;
   if (row_chunks >= 256) {
@@ -41,29 +51,29 @@ __global__ __launch_bounds__(256) void proj_quant_kernel(const uint16_t* x, int 
     more = chunk / (uint32_t)row_chunks;
     chunk -= more * row_chunks;
   }
-  const int64_t row = (int64_t)first_row + more;
-  const int at = (int)chunk * CHUNK;
-  const bool in = row < rows && at < cols;
+  constexpr int PARTS = GATE ? 2 : 1;
+  const uint32_t at = chunk * CHUNK, blocks = row_chunks / (QB / CHUNK);
+  const bool in = first_row + more < (uint32_t)rows && at < (uint32_t)cols;
   float v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = 0.f;
   if (in) {
+    const uint16_t* p = x + (int64_t)first_row * PARTS * cols + (more * PARTS * cols + at);
     if (GATE) {
-      const uint16_t* p = x + row * 2 * cols + at;
       const uint4 gw = load16(p), uw = load16(p + cols);
       float g[8], u[8];
       unpack8<DT>(gw, g);
       unpack8<DT>(uw, u);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = gated(g[i], u[i]);
+      for (int i = 0; i < 8; ++i) v[i] = gated<DT>(g[i], u[i]);
     } else {
-      unpack8<DT>(load16(x + row * cols + at), v);
+      unpack8<DT>(load16(p), v);
     }
   }
   const Quant q = quant_of(top_of_16(top_bits(v)));
   if (in) {
-    *reinterpret_cast<uint2*>(codes + row * cols + at) = codes_of(q, v);
-    if (at % QB == 0) scales[row * (row_chunks * CHUNK / QB) + at / QB] = scale_of(q);
+    *reinterpret_cast<uint2*>(codes + (int64_t)first_row * cols + (more * cols + at)) = codes_of(q, v);
+    if (at % QB == 0) scales[(int64_t)first_row * blocks + (more * blocks + at / QB)] = scale_of(q);
   }
 }
 

@@ -32,3 +32,26 @@ def test_gates_of_all_sizes(others):
     near(scales, torch.maximum(M.block_tops(y, 1) / 448, torch.tensor(2.0 ** -126, dtype=torch.float64)), GATE + 2.0 ** -24)
     held_to_quotients(codes, scales, y, GATE + 2.0 ** -24)
     untouched()
+
+
+# The result is rounded once, to 2^-24 of it.  The exponential p is off by its instruction's step of fp32 (2 x 2^-24), a rounding, and what its argument
+# leaves out (0.72 x 2^-24 at 60, the most here); that counts as p / (1 + p) of the result, and so does a rounding of the quotient's remainder.  What is of the
+# second order is below 0.05 x 2^-24 in all.  For gates from 6 on p / (1 + p) is below exp(-6).
+@pytest.mark.parametrize("lo,hi,p_counts", [(6.0, 17.0, math.exp(-6)), (-60.0, 60.0, 1.0)])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_gate_is_rounded_once(dtype, lo, hi, p_counts):
+    """A value to a row: its block's scale is fp32(value / 448), one more rounding."""
+    rows = 1 << 17
+    gu = torch.zeros((rows, 32))
+    gu[:, 5] = lo + (hi - lo) * torch.rand(rows, generator=gen(1))
+    gu[:, 16 + 5] = 1e4 * torch.exp2(torch.rand(rows, generator=gen(2)))
+    if lo < 0:
+        gu[:, 5] = gu[:, 5].clamp(min=-16 if dtype == torch.float16 else lo)
+    gu = gu.to(dtype)
+    codes, scales = fkv.empty_quant(rows, 16)
+    fkv.proj_gate(gu.cuda(), codes, scales)
+    y = M.gate(gu)[:, 5].abs()
+    off = (scales[:, 0].cpu().double() * 448 / y - 1).abs() * 2.0 ** 24
+    fine = y > 0
+    print("off by", float(off[fine].max()), "mean", float(off[fine].mean()))
+    assert off[fine].max() <= 1 + 1 + p_counts * (2 + 1 + 0.72 + 1) + 0.05
