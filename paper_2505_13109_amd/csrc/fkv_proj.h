@@ -2,6 +2,8 @@
 #pragma once
 #include "fkv_device.h"
 
+#include <tuple>
+
 namespace fkv {
 
 constexpr int QB = 128;                        // columns of a block, and rows of one of weights
@@ -34,11 +36,21 @@ struct ProjMatmul {
   int rows, n, cols;
 };
 
-void launch_proj_quant(int dtype, const uint16_t* x, int rows, int cols, int tile, uint8_t* codes, float* scales, hipStream_t st);
-void launch_proj_norm(int dtype, const ProjNorm& a, hipStream_t st);
-void launch_proj_gate(int dtype, const uint16_t* gu, int rows, int cols, uint8_t* codes, float* scales, hipStream_t st);
-void launch_proj_rope(int dtype, const ProjRope& a, hipStream_t st);
+// A launch and its own error: hipGetLastError would also say, and take away, what a call of the program's left behind.
+template <typename... P, typename... A>
+hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, const A&... args) {
+  std::tuple<P...> held(args...);
+  return std::apply([&](auto&... p) {
+    void* at[] = {&p...};
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, at, 0, st);
+  }, held);
+}
+
+hipError_t launch_proj_quant(int dtype, const uint16_t* x, int rows, int cols, int tile, uint8_t* codes, float* scales, hipStream_t st);
+hipError_t launch_proj_norm(int dtype, const ProjNorm& a, hipStream_t st);
+hipError_t launch_proj_gate(int dtype, const uint16_t* gu, int rows, int cols, uint8_t* codes, float* scales, hipStream_t st);
+hipError_t launch_proj_rope(int dtype, const ProjRope& a, hipStream_t st);
 size_t proj_matmul_work(int rows, int n, int cols);
-void launch_proj_matmul(int dtype, const ProjMatmul& a, hipStream_t st);
+hipError_t launch_proj_matmul(int dtype, const ProjMatmul& a, hipStream_t st);
 
 }  // namespace fkv

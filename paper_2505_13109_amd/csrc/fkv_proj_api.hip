@@ -16,6 +16,7 @@ int fail(int code, const char* what) {
   return code;
 }
 int hip_fail(hipError_t e, const char* what) {
+  (void)hipGetLastError();                   // (it is returned, and not left for the program's next call)
   snprintf(g_proj_error, ERR, "%s: %s", what, hipGetErrorString(e));
   return FKV_EHIP;
 }
@@ -57,8 +58,7 @@ template <typename Launch>
 int launch(int device, Launch go, const char* what) {
   OnDevice on(device);
   if (on.rc) return on.rc;
-  go();
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = go();
   return e == hipSuccess ? FKV_OK : hip_fail(e, what);
 }
 
@@ -79,7 +79,7 @@ int fkv_proj_quant(int32_t device, int32_t dtype, const void* x, int32_t rows, i
   FKV_PROJ(check(dtype, rows, cols));
   if (!fits(x) || !fits(codes) || !fits(scales)) return fail(FKV_EINVAL, "x, codes or scales: null or not 16-byte aligned");
   return launch(device, [&] {
-    launch_proj_quant(dtype, (const uint16_t*)x, rows, cols, tile, (uint8_t*)codes, scales, (hipStream_t)stream);
+    return launch_proj_quant(dtype, (const uint16_t*)x, rows, cols, tile, (uint8_t*)codes, scales, (hipStream_t)stream);
   }, "fkv_proj_quant");
 }
 
@@ -94,13 +94,13 @@ int fkv_proj_norm(int32_t device, int32_t dtype, const void* x, const void* add,
   if (!fits_or_null(add) || !fits_or_null(weight) || !fits_or_null(res) || !fits_or_null(codes) || !fits_or_null(scales) || !fits_or_null(out))
     return fail(FKV_EINVAL, "add, weight, res, codes, scales or out: not 16-byte aligned");
   ProjNorm a{(const uint16_t*)x, (const uint16_t*)add, (const uint16_t*)weight, (uint16_t*)res, (uint16_t*)out, (uint8_t*)codes, scales, rows, cols, eps};
-  return launch(device, [&] { launch_proj_norm(dtype, a, (hipStream_t)stream); }, "fkv_proj_norm");
+  return launch(device, [&] { return launch_proj_norm(dtype, a, (hipStream_t)stream); }, "fkv_proj_norm");
 }
 
 int fkv_proj_gate(int32_t device, int32_t dtype, const void* gu, int32_t rows, int32_t cols, void* codes, float* scales, void* stream) {
   FKV_PROJ(check(dtype, rows, cols));
   if (!fits(gu) || !fits(codes) || !fits(scales)) return fail(FKV_EINVAL, "gu, codes or scales: null or not 16-byte aligned");
-  return launch(device, [&] { launch_proj_gate(dtype, (const uint16_t*)gu, rows, cols, (uint8_t*)codes, scales, (hipStream_t)stream); }, "fkv_proj_gate");
+  return launch(device, [&] { return launch_proj_gate(dtype, (const uint16_t*)gu, rows, cols, (uint8_t*)codes, scales, (hipStream_t)stream); }, "fkv_proj_gate");
 }
 
 int fkv_proj_rope(int32_t device, int32_t dtype, const void* qkv, int32_t rows, int32_t n_q, int32_t n_kv, const int32_t* positions, int32_t n_axes,
@@ -115,7 +115,7 @@ int fkv_proj_rope(int32_t device, int32_t dtype, const void* qkv, int32_t rows, 
   FKV_PROJ(check(dtype, rows, D));
   if (!fits(qkv) || !fits(q) || !fits(k) || !fits(v)) return fail(FKV_EINVAL, "qkv, q, k or v: null or not 16-byte aligned");
   if (!fits(positions) || !fits(freq)) return fail(FKV_EINVAL, "positions or freq: null or not 16-byte aligned");
-  return launch(device, [&] { launch_proj_rope(dtype, a, (hipStream_t)stream); }, "fkv_proj_rope");
+  return launch(device, [&] { return launch_proj_rope(dtype, a, (hipStream_t)stream); }, "fkv_proj_rope");
 }
 
 int fkv_proj_workspace(int32_t rows, int32_t n, int32_t cols, size_t* bytes) {
@@ -136,7 +136,7 @@ int fkv_proj_matmul(int32_t device, int32_t dtype, const void* x, const float* x
   if (need && !fits(work)) return fail(FKV_EINVAL, "work: null or not 16-byte aligned");
   if (need > work_bytes) return fail(FKV_ENOMEM, "work is smaller than fkv_proj_workspace says");
   ProjMatmul a{(const uint8_t*)x, (const uint8_t*)w, xs, ws, (uint16_t*)out, (float*)work, rows, n, cols};
-  return launch(device, [&] { launch_proj_matmul(dtype, a, (hipStream_t)stream); }, "fkv_proj_matmul");
+  return launch(device, [&] { return launch_proj_matmul(dtype, a, (hipStream_t)stream); }, "fkv_proj_matmul");
 }
 
 }  // extern "C"

@@ -515,38 +515,36 @@ size_t proj_matmul_work(int rows, int n, int cols) {
   return p.g.splits > 1 ? (size_t)p.g.splits * rows * ((n + 3) / 4 * 4) * 4 : 0;
 }
 
-void launch_proj_matmul(int dtype, const ProjMatmul& a, hipStream_t st) {
+hipError_t launch_proj_matmul(int dtype, const ProjMatmul& a, hipStream_t st) {
   const Plan p = plan_of(a.rows, a.n, a.cols);
   auto go = [&](auto dt) {
     if (p.few) {
       const dim3 grid((uint32_t)ceil_div(a.n, 16 * p.nt)), block((uint32_t)p.nw * 64);
       if (a.rows <= 16) {
-        if (p.nt == 1) hipLaunchKernelGGL((proj_few_kernel<dt(), 1, 1, 16, 128>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((proj_few_kernel<dt(), 1, 2, 8, 64>), grid, block, 0, st, a);
-      } else if (a.rows <= 32) {
-        if (p.nt == 1) hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 1, 8, 128>), grid, block, 0, st, a);
-        else if (p.nt == 2) hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 2, 8, 64>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((proj_few_kernel<dt(), 2, 4, 4, 64>), grid, block, 0, st, a);
-      } else if (a.rows <= 48) {
-        hipLaunchKernelGGL((proj_few_kernel<dt(), 3, 2, 8, 64>), grid, block, 0, st, a);
-      } else {
-        hipLaunchKernelGGL((proj_few_kernel<dt(), 4, 2, 8, 64>), grid, block, 0, st, a);
+        if (p.nt == 1) return launch_kernel(proj_few_kernel<dt(), 1, 1, 16, 128>, grid, block, st, a);
+        return launch_kernel(proj_few_kernel<dt(), 1, 2, 8, 64>, grid, block, st, a);
       }
-      return;
+      if (a.rows <= 32) {
+        if (p.nt == 1) return launch_kernel(proj_few_kernel<dt(), 2, 1, 8, 128>, grid, block, st, a);
+        if (p.nt == 2) return launch_kernel(proj_few_kernel<dt(), 2, 2, 8, 64>, grid, block, st, a);
+        return launch_kernel(proj_few_kernel<dt(), 2, 4, 4, 64>, grid, block, st, a);
+      }
+      if (a.rows <= 48) return launch_kernel(proj_few_kernel<dt(), 3, 2, 8, 64>, grid, block, st, a);
+      return launch_kernel(proj_few_kernel<dt(), 4, 2, 8, 64>, grid, block, st, a);
     }
     const dim3 grid((uint32_t)std::min((int64_t)p.g.tn * p.g.tm * p.g.splits, (int64_t)TILES[p.tile].slots * CUS));
     auto many = [&](auto split) {
-      if (p.tile == 0) hipLaunchKernelGGL((proj_many_kernel<dt(), 64, 64, 1, 4, 4, 16, split()>), grid, dim3(256), 0, st, a, p.g);
-      else if (p.tile == 1) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 4, 4, 16, split()>), grid, dim3(512), 0, st, a, p.g);
-      else if (p.tile == 2) hipLaunchKernelGGL((proj_many_kernel<dt(), 128, 128, 2, 2, 2, 8, split()>), grid, dim3(256), 0, st, a, p.g);
-      else hipLaunchKernelGGL((proj_many_kernel<dt(), 256, 256, 2, 4, 2, 8, split()>), grid, dim3(512), 0, st, a, p.g);
+      if (p.tile == 0) return launch_kernel(proj_many_kernel<dt(), 64, 64, 1, 4, 4, 16, split()>, grid, dim3(256), st, a, p.g);
+      if (p.tile == 1) return launch_kernel(proj_many_kernel<dt(), 128, 128, 2, 4, 4, 16, split()>, grid, dim3(512), st, a, p.g);
+      if (p.tile == 2) return launch_kernel(proj_many_kernel<dt(), 128, 128, 2, 2, 2, 8, split()>, grid, dim3(256), st, a, p.g);
+      return launch_kernel(proj_many_kernel<dt(), 256, 256, 2, 4, 2, 8, split()>, grid, dim3(512), st, a, p.g);
     };
     if (p.g.splits == 1) return many(std::false_type());
-    many(std::true_type());
-    hipLaunchKernelGGL((proj_join_kernel<dt()>), dim3((uint32_t)ceil_div((int64_t)a.rows * ((a.n + 3) / 4), 256)), dim3(256), 0, st, a, p.g.splits);
+    const hipError_t e = many(std::true_type());
+    if (e != hipSuccess) return e;
+    return launch_kernel(proj_join_kernel<dt()>, dim3((uint32_t)ceil_div((int64_t)a.rows * ((a.n + 3) / 4), 256)), dim3(256), st, a, p.g.splits);
   };
-  if (dtype == 0) go(std::integral_constant<int, 0>());
-  else go(std::integral_constant<int, 1>());
+  return dtype == 0 ? go(std::integral_constant<int, 0>()) : go(std::integral_constant<int, 1>());
 }
 
 }  // namespace fkv

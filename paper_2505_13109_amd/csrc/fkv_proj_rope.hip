@@ -63,19 +63,18 @@ __global__ __launch_bounds__(NT) void proj_rope_kernel(ProjRope a) {
 // Rows a block so that its threads have work, where a row has few heads: 16384 rows of 4 + 2 heads 9.9 us with 4 rows and 256 threads, 18.7 with
 // one row and 512; 8 + 2 heads 14.9 with 4 rows, 16.1 with 2, 21.3 with one; 16 + 8 heads 38.4 with 2, 39.2 with 4, 40.3 with one; 28 + 8 heads
 // 53.3 with one, 55.5 with 2, 56.9 with 4.
-void launch_proj_rope(int dtype, const ProjRope& a, hipStream_t st) {
+hipError_t launch_proj_rope(int dtype, const ProjRope& a, hipStream_t st) {
   const int heads = a.n_q + 2 * a.n_kv;
   auto go = [&](auto dt) {
     auto with = [&](auto rb, auto nt) {
-      hipLaunchKernelGGL((proj_rope_kernel<dt(), rb(), nt()>), dim3(((uint32_t)a.rows + rb() - 1) / rb()), dim3(nt()), 0, st, a);
+      return launch_kernel(proj_rope_kernel<dt(), rb(), nt()>, dim3(((uint32_t)a.rows + rb() - 1) / rb()), dim3(nt()), st, a);
     };
-    if (heads <= 8) with(std::integral_constant<int, 4>(), std::integral_constant<int, 256>());
-    else if (heads <= 12) with(std::integral_constant<int, 4>(), std::integral_constant<int, 512>());
-    else if (heads <= 24) with(std::integral_constant<int, 2>(), std::integral_constant<int, 512>());
-    else with(std::integral_constant<int, 1>(), std::integral_constant<int, 512>());
+    if (heads <= 8) return with(std::integral_constant<int, 4>(), std::integral_constant<int, 256>());
+    if (heads <= 12) return with(std::integral_constant<int, 4>(), std::integral_constant<int, 512>());
+    if (heads <= 24) return with(std::integral_constant<int, 2>(), std::integral_constant<int, 512>());
+    return with(std::integral_constant<int, 1>(), std::integral_constant<int, 512>());
   };
-  if (dtype == 0) go(std::integral_constant<int, 0>());
-  else go(std::integral_constant<int, 1>());
+  return dtype == 0 ? go(std::integral_constant<int, 0>()) : go(std::integral_constant<int, 1>());
 }
 
 }  // namespace fkv

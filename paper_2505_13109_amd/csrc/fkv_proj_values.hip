@@ -224,53 +224,50 @@ __global__ __launch_bounds__(NT) void proj_norm_kernel(ProjNorm a) {
 }
 
 template <typename F>
-void by_type(int dtype, F f) {
-  if (dtype == 0) f(std::integral_constant<int, 0>());
-  else f(std::integral_constant<int, 1>());
+hipError_t by_type(int dtype, F f) {
+  return dtype == 0 ? f(std::integral_constant<int, 0>()) : f(std::integral_constant<int, 1>());
 }
 template <typename F>
-void by_flag(bool flag, F f) {
-  if (flag) f(std::true_type());
-  else f(std::false_type());
+hipError_t by_flag(bool flag, F f) {
+  return flag ? f(std::true_type()) : f(std::false_type());
 }
 
 }  // namespace
 
-void launch_proj_quant(int dtype, const uint16_t* x, int rows, int cols, int tile, uint8_t* codes, float* scales, hipStream_t st) {
+hipError_t launch_proj_quant(int dtype, const uint16_t* x, int rows, int cols, int tile, uint8_t* codes, float* scales, hipStream_t st) {
   const int blocks = blocks_of(cols);
-  by_type(dtype, [&](auto dt) {
+  return by_type(dtype, [&](auto dt) {
     if (tile == 1) {
       const int64_t n = (int64_t)rows * blocks * (QB / CHUNK);
-      hipLaunchKernelGGL((proj_quant_kernel<dt(), false>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, st, x, rows, blocks * (QB / CHUNK), cols, codes, scales);
-    } else {
-      hipLaunchKernelGGL((proj_quant_tile_kernel<dt()>), dim3((uint32_t)blocks * blocks_of(rows)), dim3(256), 0, st, x, rows, cols, blocks, codes, scales);
+      return launch_kernel(proj_quant_kernel<dt(), false>, dim3((uint32_t)((n + 255) / 256)), dim3(256), st, x, rows, blocks * (QB / CHUNK), cols, codes, scales);
     }
+    return launch_kernel(proj_quant_tile_kernel<dt()>, dim3((uint32_t)blocks * blocks_of(rows)), dim3(256), st, x, rows, cols, blocks, codes, scales);
   });
 }
 
-void launch_proj_gate(int dtype, const uint16_t* gu, int rows, int cols, uint8_t* codes, float* scales, hipStream_t st) {
+hipError_t launch_proj_gate(int dtype, const uint16_t* gu, int rows, int cols, uint8_t* codes, float* scales, hipStream_t st) {
   const int blocks = blocks_of(cols);
   const int64_t n = (int64_t)rows * blocks * (QB / CHUNK);
-  by_type(dtype, [&](auto dt) {
-    hipLaunchKernelGGL((proj_quant_kernel<dt(), true>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, st, gu, rows, blocks * (QB / CHUNK), cols, codes, scales);
+  return by_type(dtype, [&](auto dt) {
+    return launch_kernel(proj_quant_kernel<dt(), true>, dim3((uint32_t)((n + 255) / 256)), dim3(256), st, gu, rows, blocks * (QB / CHUNK), cols, codes, scales);
   });
 }
 
 // A block's threads are the fewest that hold a row, up to 512 with two chunks each: 8192 rows of 1024 columns 12.5 us with 128 threads, 23.8 with 512,
 // 32.6 with 512 that have two; 8192 x 2048 24.3 with 256, 28.8 and 35.4; 4096 x 8192 45 with 512 x 2, 46 with 1024, 49 with 256.  Rows that
 // are longer are gone through twice, 1024 threads at a time (64 x 32768 9.3 us, 512 x 2 10.5).  One row takes 2.4 to 3.6 us up to 8192.
-void launch_proj_norm(int dtype, const ProjNorm& a, hipStream_t st) {
-  by_type(dtype, [&](auto dt) {
-    by_flag(a.add != nullptr, [&](auto add) {
-      by_flag(a.out != nullptr, [&](auto out) {
+hipError_t launch_proj_norm(int dtype, const ProjNorm& a, hipStream_t st) {
+  return by_type(dtype, [&](auto dt) {
+    return by_flag(a.add != nullptr, [&](auto add) {
+      return by_flag(a.out != nullptr, [&](auto out) {
         auto go = [&](auto nt, auto ch) {
-          hipLaunchKernelGGL((proj_norm_kernel<dt(), nt(), ch(), add(), out()>), dim3((uint32_t)a.rows), dim3(nt()), 0, st, a);
+          return launch_kernel(proj_norm_kernel<dt(), nt(), ch(), add(), out()>, dim3((uint32_t)a.rows), dim3(nt()), st, a);
         };
-        if (a.cols <= 1024) go(std::integral_constant<int, 128>(), std::integral_constant<int, 1>());
-        else if (a.cols <= 2048) go(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-        else if (a.cols <= 4096) go(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
-        else if (a.cols <= 8192) go(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
-        else go(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
+        if (a.cols <= 1024) return go(std::integral_constant<int, 128>(), std::integral_constant<int, 1>());
+        if (a.cols <= 2048) return go(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
+        if (a.cols <= 4096) return go(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
+        if (a.cols <= 8192) return go(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
+        return go(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
       });
     });
   });
