@@ -97,7 +97,7 @@ class DecoderStack:
     def step(self, x, external_qkv=None, stream=None, positions=None):
         """x [batch, hidden] -> [batch, hidden].  external_qkv: per layer (q [batch,n_q,d], k, v [batch,n_kv,d]).
         positions (fp8 only): rotary positions of the tokens, [batch] or [axes, batch] int32 on the GPU; None: their places in the sequences, on
-        every axis.
+        every axis (over a FreeKV context, each layer's own).
 
         Over a PagedCache the whole step runs on `stream`, behind what the current stream has been given and before what it is given next:
         positions come from the device, so the projections have to follow the cache's calls.  Over a FreeKV context, `stream` is the one that
@@ -149,9 +149,9 @@ class DecoderStack:
         if self.paged:
             self.fkv.extend(self.seqs, stream=stream)
             self.fkv.tables(self.seqs, self.lens, stream=stream)
-        if positions is None:
-            places = self.lens - 1 if self.paged else torch.full_like(self.positions, self.fkv.context_len(0))
-            positions = places if self.sections is None else places.expand(1 + max(self._axes()), -1).contiguous()
+        given, place_before = positions, None
+        if given is None and self.paged:
+            positions = self._on_all_axes(self.lens - 1)
         y = None
         for layer in range(self.n_layers):
             if y is None:
@@ -160,6 +160,10 @@ class DecoderStack:
                 proj_norm(x, None, *self.h8, add=y, res=self.x[0])
                 x = self.x[0]
             proj_matmul(*self.h8, *self.wqkv[layer], self.qkv)
+            if given is None and not self.paged:
+                place = self.fkv.context_len(layer)                 # (the layers of one model share it)
+                if place != place_before:
+                    positions, place_before = self._on_all_axes(torch.full_like(self.positions, place)), place
             q, k, v = self.heads[layer]
             proj_rope(self.qkv.view(self.batch, self.n_q + 2 * self.n_kv, self.d), positions, self.inv_freq, q, k, v, sections=self.sections)
             if external_qkv is not None:
@@ -179,6 +183,10 @@ class DecoderStack:
             proj_matmul(*self.f8, *self.wd[layer], self.y)
             y = self.y
         return x + y
+
+    def _on_all_axes(self, places):
+        """[batch] positions as they are, or the same on each of the axes."""
+        return places if self.sections is None else places.expand(1 + max(self._axes()), -1).contiguous()
 
     def _axes(self):
         s = list(self.sections)

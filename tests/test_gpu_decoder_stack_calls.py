@@ -1,0 +1,37 @@
+"""DecoderStack with weights in 8 bits, beside its arithmetic: layers of different lengths, what it hands out, calls that it refuses."""
+import pytest
+import torch
+
+import paper_2505_13109_amd as fkv
+import proj_model as M
+from paper_2505_13109_amd.layer_loop import DecoderStack
+from test_gpu_decoder_stack_fp8 import stack_of
+from test_gpu_paged_cache import D, Pair, ints
+
+pytestmark = pytest.mark.gpu
+
+
+def test_layers_of_different_lengths():
+    """Each layer's own length is its token's position, as with weights in 16 bits."""
+    lens = [520, 713, 520]
+    g = fkv.FreeKV(n_layers=3, batch=2, n_q_heads=8, n_kv_heads=2, max_ctx=2048, budget=512, sink=64, window=64, tau=0.8, dtype="bf16", placement=0)
+    gen = torch.Generator().manual_seed(1)
+    for layer, n in enumerate(lens):
+        g.load_prefix(layer, *(torch.randn((2, n, 2, D), generator=gen).bfloat16().cuda() for _ in "kv"))
+    x = torch.randn((2, 8 * D), generator=gen).bfloat16().cuda()
+    for n_layers in (1, 2, 3):                                # the last of them left its product behind
+        stack = DecoderStack(g, weights="fp8", ffn_mult=1.0)
+        stack.n_layers = n_layers
+        stack.step(x)
+        q, k, v = stack.last_qkv[n_layers - 1]
+        at = torch.full((2,), lens[n_layers - 1], dtype=torch.int32)
+        wq, wk, wv, oq, ok = M.rope(stack.qkv.cpu().view(2, 12, D), at, stack.inv_freq.cpu(), 8, 2)
+        for got, want, off in ((q, wq, oq), (k, wk, ok)):
+            err = (got.cpu().double() - want).abs() - torch.finfo(torch.bfloat16).eps / 2 * 1.01 * want.abs() - off
+            assert (err <= 0).all(), (n_layers, float(err.max()))
+        assert torch.equal(v.cpu().double(), wv)
+        for layer in range(n_layers):
+            lens[layer] += 1
+            assert g.context_len(layer) == lens[layer]
+    torch.cuda.synchronize()
+    g.close()
