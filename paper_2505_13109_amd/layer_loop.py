@@ -76,7 +76,6 @@ class DecoderStack:
             self.h8, self.f8 = (empty_quant(self.batch, cols, device=dev) for cols in (self.hidden, self.ffn))
             self.qkv, self.gu, self.y = new(self.batch, qkv_out), new(self.batch, 2 * self.ffn), new(self.batch, self.hidden)
             self.x = new(2, self.batch, self.hidden)         # the stream of a layer, before and behind the attention
-            self.heads = [tuple(new(self.batch, n, self.d) for n in (self.n_q, self.n_kv, self.n_kv)) for _ in range(self.n_layers)]
             self.positions = new(self.batch, dtype=torch.int32)
 
     @staticmethod
@@ -164,7 +163,8 @@ class DecoderStack:
                 place = self.fkv.context_len(layer)                 # (the layers of one model share it)
                 if place != place_before:
                     positions, place_before = self._on_all_axes(torch.full_like(self.positions, place)), place
-            q, k, v = self.heads[layer]
+            # (the step's own, as last_qkv hands them out)
+            q, k, v = (torch.empty((self.batch, n, self.d), dtype=self.dtype, device=x.device) for n in (self.n_q, self.n_kv, self.n_kv))
             proj_rope(self.qkv.view(self.batch, self.n_q + 2 * self.n_kv, self.d), positions, self.inv_freq, q, k, v, sections=self.sections)
             if external_qkv is not None:
                 q, k, v = external_qkv[layer]

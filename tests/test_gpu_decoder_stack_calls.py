@@ -35,3 +35,18 @@ def test_layers_of_different_lengths():
             assert g.context_len(layer) == lens[layer]
     torch.cuda.synchronize()
     g.close()
+
+
+def test_a_steps_queries_keys_and_values_stay():
+    """What a step has handed out is not written again by those behind it."""
+    p = Pair(n_layers=2, n_kv=2, G=4, max_seqs=2, max_ctx=256, n_pages=16)
+    p.grow([0, 1], [20, 9])
+    stack = stack_of(p, [0, 1], ffn_mult=1.0)
+    x = torch.randn((2, 8 * D), generator=p.gen).bfloat16().cuda()
+    kept = []
+    for _ in range(3):
+        x = stack.step(x)
+        kept.append([(t, t.clone()) for layer in stack.last_qkv for t in layer])
+    torch.cuda.synchronize()
+    for step in kept:
+        assert len(step) == 6 and all(torch.equal(t, then) for t, then in step)
