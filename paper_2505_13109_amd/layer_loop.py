@@ -26,7 +26,7 @@ import torch
 
 from .binding import FreeKV
 from .paged_cache import PagedCache
-from .projection import empty_quant, proj_gate, proj_matmul, proj_norm, proj_quant, proj_rope
+from .projection import MAX_AXES, axes_of, empty_quant, proj_gate, proj_matmul, proj_norm, proj_quant, proj_rope
 
 
 class DecoderStack:
@@ -38,6 +38,7 @@ class DecoderStack:
             raise ValueError(f"weights: None or 'fp8' are known, not {weights!r}")
         if rope_sections is not None and weights is None:
             raise ValueError("positions of several axes go with weights='fp8'")
+        self.axes = 1 if rope_sections is None else axes_of(rope_sections)          # (refuses sections that no step could do with)
         self.fkv, self.seqs = fkv, seqs
         self.paged = isinstance(fkv, PagedCache)
         if self.paged != (seqs is not None):
@@ -103,6 +104,8 @@ class DecoderStack:
         its calls are launched on; the rest runs on the current stream, which has to be the same."""
         if self.weights is None and positions is not None:
             raise ValueError("positions of the caller's go with weights='fp8'")
+        if self.weights is not None:
+            self._refuse_step(x, positions)
         run = self._step if self.weights is None else lambda *a: self._step_in_8_bits(*a, positions)
         here = torch.cuda.current_stream(self.fkv.device) if self.paged and stream is not None else None
         if here is None or stream == here:
@@ -184,10 +187,20 @@ class DecoderStack:
             y = self.y
         return x + y
 
+    def _refuse_step(self, x, positions):
+        """What a kernel of the step would refuse, before the sequences have a token more."""
+        dev = self.inv_freq.get_device()
+        if not (isinstance(x, torch.Tensor) and x.dtype is self.dtype and x.shape == (self.batch, self.hidden) and x.get_device() == dev and x.is_contiguous()
+                and x.data_ptr() % 16 == 0):
+            raise ValueError(f"x: a contiguous {self.dtype} tensor of shape {(self.batch, self.hidden)} on cuda:{dev}, 16-byte aligned, is wanted")
+        if positions is None:
+            return
+        shape = tuple(positions.shape) if isinstance(positions, torch.Tensor) else None
+        axes = 1 if shape == (self.batch,) else shape[0] if shape and shape[1:] == (self.batch,) else 0
+        if not (self.axes <= axes <= MAX_AXES and positions.dtype is torch.int32 and positions.get_device() == dev and positions.is_contiguous()):
+            raise ValueError(f"positions: a contiguous int32 tensor on cuda:{dev} is wanted, [axes, {self.batch}] with {self.axes} to {MAX_AXES} axes"
+                             + (f", or [{self.batch}]" if self.axes == 1 else ""))
+
     def _on_all_axes(self, places):
         """[batch] positions as they are, or the same on each of the axes."""
-        return places if self.sections is None else places.expand(1 + max(self._axes()), -1).contiguous()
-
-    def _axes(self):
-        s = list(self.sections)
-        return s if len(s) == 64 else range(len(s))
+        return places if self.sections is None else places.expand(self.axes, -1).contiguous()

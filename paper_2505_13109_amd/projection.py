@@ -16,6 +16,7 @@ import torch
 from .binding import FreeKVError, lib
 
 BLOCK = 128
+MAX_AXES = 4
 FEW_ROWS = 32                 # up to here a product needs no workspace
 CODES = torch.float8_e4m3fn
 F32, I32 = torch.float32, torch.int32
@@ -183,6 +184,16 @@ def _axis_of(sections, axes):
             _axes_known.clear()
         known = _axes_known[key] = (C.c_int32 * 64)(*each)
     return known
+
+
+def axes_of(sections):
+    """How many axes' positions `sections` need; refuses what proj_rope would."""
+    each = tuple(sections)
+    axes = 1 + max(each) if len(each) == 64 else len(each)
+    if axes > MAX_AXES:
+        raise FreeKVError(f"sections: {axes} axes, {MAX_AXES} are the most")
+    _axis_of(each, axes)
+    return axes
 
 
 def proj_matmul(codes, scales, w, w_scales, out, stream=None):

@@ -50,3 +50,27 @@ def test_a_steps_queries_keys_and_values_stay():
     torch.cuda.synchronize()
     for step in kept:
         assert len(step) == 6 and all(torch.equal(t, then) for t, then in step)
+
+
+def test_a_refused_step_leaves_the_cache_as_it_was():
+    p = Pair(n_layers=1, n_kv=2, G=4, max_seqs=2, max_ctx=256, n_pages=16)
+    p.grow([0, 1], [20, 9])
+    one, three = stack_of(p, [0, 1], ffn_mult=1.0), stack_of(p, [0, 1], ffn_mult=1.0, rope_sections=(16, 24, 24))
+    x = torch.randn((2, 8 * D), generator=p.gen).bfloat16().cuda()
+    at = ints([20, 9])
+    for bad in (x[:1], x.half(), x.cpu(), x[:, :512], x.T.contiguous().T, None):
+        for stack in (one, three):
+            with pytest.raises((ValueError, fkv.FreeKVError)):
+                stack.step(bad)
+    for stack, bad in ((one, at.long()), (one, at[:1]), (one, at.cpu()), (one, at.view(2, 1)), (one, at.repeat(5).view(5, 2)), (one, 20), (three, at),
+                       (three, at.repeat(2).view(2, 2)), (three, at.repeat(3).view(2, 3).T)):
+        with pytest.raises((ValueError, fkv.FreeKVError)):
+            stack.step(x, positions=bad)
+    torch.cuda.synchronize()
+    p.check_tables()
+    p.check_contents()
+    given, own = one.step(x, positions=at), one.step(x)                  # (each appends a token)
+    assert torch.isfinite(given.float()).all() and torch.isfinite(own.float()).all()
+    for sections in ((16, 24), (70, -6), [4] * 64, [-1] + [0] * 63, (16, 16, 16, 8, 8)):
+        with pytest.raises((ValueError, fkv.FreeKVError)):
+            stack_of(p, [0, 1], ffn_mult=1.0, rope_sections=sections)
