@@ -140,7 +140,7 @@ def proj_gate(gu, codes, scales, stream=None):
 def proj_rope(qkv, positions, freq, q, k, v, sections=None, stream=None):
     """qkv [rows, n_q + 2 n_kv, 128] apart into q, k, v, q and k turned by positions ([rows] or [axes, rows] int32) times freq ([64] fp32).
     sections: how many pairs of channels each axis has, one axis behind the other (64 in all), or each pair's axis (64 numbers); None: all the
-    first axis'."""
+    first axis'.  positions and freq may begin at any of their numbers; the other tensors on 16 bytes, as everywhere here."""
     rows, heads, d = _shape(qkv, 3)
     n_q, n_kv = (q.shape[1], k.shape[1]) if isinstance(q, torch.Tensor) and isinstance(k, torch.Tensor) and q.dim() == k.dim() == 3 else (0, 0)
     dev = _device(qkv)
@@ -160,8 +160,13 @@ def proj_rope(qkv, positions, freq, q, k, v, sections=None, stream=None):
         _refuse(("qkv", qkv, _TYPES, (rows, n_q + 2 * n_kv, 128), dev), ("q", q, types, (rows, n_q, 128), dev), ("k", k, types, (rows, n_kv, 128), dev),
                 ("v", v, types, (rows, n_kv, 128), dev), ("positions", positions, (I32,), (axes, rows) if axes else (rows,), dev), ("freq", freq, (F32,), (64,), dev))
     axes = axes or 1
-    rc = lib().fkv_proj_rope(dev, _TYPES[dtype], qkv.data_ptr(), rows, n_q, n_kv, positions.data_ptr(), axes, None if sections is None else _axis_of(sections, axes),
-                             freq.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), _stream(stream, dev))
+    at, by = positions.data_ptr(), freq.data_ptr()
+    if (at | by) & 15:           # (one step's of a tensor of all steps', say: the stream takes a copy to where the entry point wants it)
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            positions, freq = (t.clone() if t.data_ptr() & 15 else t for t in (positions, freq))
+        at, by = positions.data_ptr(), freq.data_ptr()
+    rc = lib().fkv_proj_rope(dev, _TYPES[dtype], qkv.data_ptr(), rows, n_q, n_kv, at, axes, None if sections is None else _axis_of(sections, axes),
+                             by, q.data_ptr(), k.data_ptr(), v.data_ptr(), _stream(stream, dev))
     if rc:
         _failed(rc, "fkv_proj_rope")
 
