@@ -11,7 +11,7 @@
  * Conventions are those of freekv.h: 0 or a negative FKV_E* code, `stream` a hipStream_t, device pointers, tensors contiguous and 16-byte
  * aligned.  T is the storage type, FKV_DTYPE_*.  The calls keep no state and only enqueue kernels, on `device`, whichever is current; calls on several
  * streams may run at once, and any of them may be captured into a graph.  rows: 0 to 4194304, 0 does nothing.  cols: multiples of 16 up
- * to 131072, and rows times ceil(cols / 128) below 2^28.
+ * to 131072, and rows times ceil(cols / 128) at most 2^28 - 16.
  */
 #ifndef FREEKV_PROJ_H
 #define FREEKV_PROJ_H

@@ -44,8 +44,8 @@ int check(int dtype, int rows, int cols) {
   if (dtype != FKV_DTYPE_FP16 && dtype != FKV_DTYPE_BF16) return fail(FKV_EINVAL, "dtype must be fp16 or bf16");
   if (rows < 0 || rows > PROJ_MAX_ROWS) return fail(FKV_ERANGE, "rows must be 0 to 4194304");
   if (cols < 16 || cols > PROJ_MAX_COLS || cols % 16) return fail(FKV_ERANGE, "cols must be a multiple of 16 up to 131072");
-  // (a launch has fewer than 2^32 threads)
-  if ((int64_t)rows * blocks_of(cols) >= 1 << 28) return fail(FKV_ERANGE, "rows x ceil(cols / 128) must be below 268435456");
+  // (16 threads each, in blocks of 256: a launch has fewer than 2^32)
+  if ((int64_t)rows * blocks_of(cols) > (1 << 28) - 16) return fail(FKV_ERANGE, "rows x ceil(cols / 128) must be at most 268435440");
   return rows == 0;
 }
 int check_n(int rows, int n) {
