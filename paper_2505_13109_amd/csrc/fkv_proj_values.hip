@@ -42,7 +42,7 @@ __device__ __forceinline__ float gated(float g, float u) {
 template <int DT, bool GATE>
 __global__ __launch_bounds__(256) void proj_quant_kernel(const uint16_t* x, int rows, int row_chunks, int cols, uint8_t* codes, float* scales) {
   // row_chunks: chunks of a row, up to the end of its last block.  Where a block begins is divided once, not for each thread, and what
-  // lies before it in memory is the same for all: a thread's own offsets, of at most 255 rows of 2048 columns or one longer one, have 32 bits.
+  // lies before it in memory is the same for all: a thread's own offsets, of 16 rows at most, have 32 bits.
   const uint32_t first = blockIdx.x * 256u, first_row = first / (uint32_t)row_chunks;
   uint32_t chunk = first - first_row * row_chunks + threadIdx.x, more = 0;
   if (row_chunks >= 256) {
