@@ -1,12 +1,12 @@
 /* freekv_proj.h -- a decoder layer's projections in 8 bits, around the retrieval loop (freekv.h) and the paged cache (freekv_cache.h).
  *
  * What a layer does between a cache's calls: the residual's addition and the norm, products with weights, rotary positions, the gated
- * activation.  Weights and the activations that meet them are kept in 8 bits, a third of a decode step's bytes:
+ * activation.  Weights and the activations that meet them are kept in 8 bits, half the bytes of 16:
  *     a block is 128 columns of one row (activations), or of 128 rows (weights); what is left at the ends makes smaller blocks
  *     scale = max(fp32(max |x| / 448), 2^-126)      over a block
  *     code  = e4m3(fp32(x / scale))                 both rounded to nearest, ties to even; e4m3 as in the OCP's format, largest 448
- * and code times scale is what a value stands for.  A block that holds a NaN or an infinity stands for NaN: its scale is one, its codes
- * are 0.  Codes are [rows, cols] bytes, scales fp32 [rows (weights: ceil(rows / 128)), ceil(cols / 128)].
+ * and code times scale is what a value stands for.  A block that holds a NaN or an infinity stands for NaN: its scale is a NaN, its
+ * codes are 0.  Codes are [rows, cols] bytes, scales fp32 [rows (weights: ceil(rows / 128)), ceil(cols / 128)].
  *
  * Conventions are those of freekv.h: 0 or a negative FKV_E* code, `stream` a hipStream_t, device pointers, tensors contiguous and 16-byte
  * aligned.  T is the storage type, FKV_DTYPE_*.  The calls keep no state and only enqueue kernels, on `device`, whichever is current; calls on several
@@ -47,14 +47,16 @@ int fkv_proj_gate(int32_t device, int32_t dtype, const void* gu_dev, int32_t row
  *     qkv dev [rows, n_q + 2 n_kv, 128] of T -> q [rows, n_q, 128], k, v [rows, n_kv, 128]
  *     channels i and i + 64 of a head (i < 64) turn by the angle positions[axis_of[i]][row] freq[i]; v is copied
  * positions dev [n_axes, rows] i32, any sign; freq dev [64] fp32; axis_of HOST [64], NULL: all of the first axis.  n_axes: 1 to 4.
- * The angle is the exact product taken off whole turns in fp64, so far positions turn as exactly as near ones; results are rounded once. */
+ * The product is taken in fp64 and whole turns off it there: it is exact for positions below 2^29, which turn as exactly as near ones, and beyond that off
+ * by at most 2^-53 of the angle (2^-23 of a radian at frequencies to 1).  Results are rounded once. */
 int fkv_proj_rope(int32_t device, int32_t dtype, const void* qkv_dev, int32_t rows, int32_t n_q, int32_t n_kv, const int32_t* positions_dev, int32_t n_axes,
                   const int32_t* axis_of, const float* freq_dev, void* q_dev, void* k_dev, void* v_dev, void* stream);
 
 /* out[r, c] = T(sum_b scale_x[r, b] scale_w[c / 128, b] sum_{i in block b} x[r, i] w[c, i]):
  * x codes [rows, cols] with a scale for each row's block, w codes [n, cols] with one for each 128 x 128, out [rows, n] of T, n: 1 to 4194304,
- * rows times n at most 2^37.  Sums are in fp32, their order is fixed by the sizes.  Up to 32 rows the products that they are of are exact; beyond, the 8-bit
- * matrix instruction cuts products at 2^-13 of the largest of eight adjacent columns before it adds them.  Where the product of two scales is below 2^-126
+ * rows times n at most 2^37.  Sums are in fp32, their order is fixed by the sizes.  Up to 32 rows, and up to 64 where n and cols are at
+ * most 8192, the products that they are of are exact; else the 8-bit matrix instruction cuts products at 2^-13 of the largest of eight adjacent columns before
+ * it adds them, which moves a sum of 4096 normal products by some 1e-4 of its size.  Where the product of two scales is below 2^-126
  * digits are lost, beyond fp32's largest it is infinite (NaN where it meets a sum of 0).
  * work_dev: at least fkv_proj_workspace's bytes, this call's until the stream is done with it; NULL where they are 0, as they are up to 32 rows. */
 int fkv_proj_matmul(int32_t device, int32_t dtype, const void* x_dev, const float* x_scales_dev, const void* w_dev, const float* w_scales_dev, int32_t rows,

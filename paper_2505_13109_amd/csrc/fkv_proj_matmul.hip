@@ -36,7 +36,8 @@ __device__ __forceinline__ void store4(uint16_t* out, int64_t row, int c, int n,
 
 // ---- codes into LDS ------------------------------------------------------------------------------------------------
 
-// 16 bytes of each lane into LDS behind each other, from `at` on; zeros where an offset is past the buffer's end
+// 16 bytes of each lane into LDS behind each other, from `at` on; zeros where an offset is past the buffer's end.  (The compiler
+// reserves m0 and sets it right before uses of its own; it takes no clobber of it.)
 __device__ __forceinline__ void load_lds(const int4v& buffer, uint32_t offset, uint32_t at) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
 }
@@ -470,7 +471,10 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // The tiles that many rows are cut into, and what they cost, in us: a block of 128 columns where a compute unit has one of them and where it has
 // two, and a tile's results.  From products of 48 to 2048 rows (n x cols of 4096 x 11056 and x 14336, 6144 and 28672 x 4096, 8192 x 8192,
-// 1 to 16 parts), whose times these give within 8 %; what they choose took at most 10 % longer than the best of all, 1 or 2 % as a rule.
+// 1 to 16 parts), whose times these give within 8 %; what they choose took at most 10 % longer than the best of all, 1 or 2 % as a rule.  All of those
+// have long axes: activations' and results' bytes are not counted, so where results are most of the bytes the tiles are too few and too large
+// (1000 x 9008 x 256 10.9 us, 500 x 16384 x 192 8.6, both 4.0 of bytes; where n is no multiple of 8 stores are of 2 or 8 bytes, too, and 1000 x 9001 x 256
+// takes 27.8, 500 x 16385 x 192 24.8).
 constexpr struct { int tn, tm, slots; float one, two, results; } TILES[] = {
     {64, 64, 2, 0.40f, 0.58f, 0.f}, {128, 128, 1, 0.72f, 0.72f, 2.f}, {128, 128, 2, 1.28f, 1.35f, 1.f}, {256, 256, 1, 2.0f, 2.0f, 0.f}};
 constexpr float READ_RATE = 4.5e6f, JOIN = 3.f, JOIN_RATE = 5.5e6f;       // bytes a us of weights, us of a join's launch, bytes a us of parts
@@ -480,7 +484,8 @@ constexpr int MAX_PARTS = 16, LEAST_PART = 4;
 // more than 16 rows where there are blocks for all compute units all the same (32 rows x 28672 x 4096 27.6 us, two 29.3; 32 x 6144 x 4096 12.9 and
 // 9.8), but one, with more waves, where few columns are long (16 rows x 4096 x 14336 14.8 us, two 18.3).  Beyond 32 rows that is faster than
 // tiles while a block a compute unit has all columns and they are not long (48 x 6144 x 4096 10.9 us, tiles 15.2; 48 x 4096 x 14336 26 and 22;
-// 48 x 28672 x 4096 37.5 and 35).
+// 48 x 28672 x 4096 37.5 and 35).  The axis is not cut: 4096 x 4096 has 128 blocks (1 row 5.6 us, 32 rows 6.5; the bytes are 3.3), and few columns of a long axis
+// have few blocks that go all along it (512 x 28672 10.0 us for one row, 13.3 for 16, 18.7 for 32; the bytes are 3.0).
 Plan plan_of(int rows, int n, int cols) {
   Plan p{};
   const int blocks = blocks_of(cols);
